@@ -32,9 +32,9 @@
 #include <math.h>
 
 #include <atomic>
-#include <mutex>
 
 #include "common.cuh"
+#include "tiles.cuh"
 #include "trace.cuh"
 
 namespace cg = cooperative_groups;
@@ -44,13 +44,10 @@ namespace sagekv {
 constexpr int kDecodeThreads = (kDecodeWarps + 1) * 32;   // eight consumer warps and the warp that issues the copies
 constexpr int kConsumerThreads = kDecodeWarps * 32;
 constexpr int kDecodeBaseCluster = 8;          // the cluster size tried first (the portable limit)
-constexpr int kSlotBytes = 16 * 256;           // a slot of the staging area: 16 rows of K or of V
-constexpr int kHalfBytes = 16 * 128;           // 16 rows x 64 columns: one box of the tensor copy
 constexpr int kPHeadWords = 12;                // 32-bit words per (tile, head) of the weight buffer: 8 used, 4 spread the banks
 constexpr int kPTileWords = kMaxGroup * kPHeadWords;
 constexpr int kQkGroup = 3;                    // tiles of the first product a warp works on at once
 constexpr int kQkTiles = (kDecodeMaxTiles + kDecodeWarps - 1) / kDecodeWarps;   // tiles a warp may get in the first product (6)
-constexpr uint32_t kWaitLimit = 1u << 22;      // polls of a copy barrier before giving up (each poll already blocks for a while)
 
 struct DecShared {
   // softmax weights: [tile][head][row pair g: rows 2g, 2g + 1]; the tensor-memory variant keeps its two small
@@ -69,64 +66,6 @@ struct DecShared {
   float2 inbox_ml[kDecodeMaxCluster][kMaxGroup];               // [source CTA][head] (max, sum)
   float inbox_o[(kHeadDim + 4 * kDecodeMaxCluster) * kMaxGroup];   // [source CTA][my column][head]; cluster size x columns <= 160
 };
-
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// false: the wait ran out
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kWaitLimit; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
-  return false;
-}
-
-// one box of a [batch, head, row, column] bf16 tensor -> shared memory; the copy reads this GPU's memory only
-// (the cache rows are read once per call: they are marked evict-first in L2, so that the small operands every
-// call reads after its dependency wait, q and the step counter, tend to stay there)
-__device__ __forceinline__ void tensor_copy_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar,
-                                               uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;"
-      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr));
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr));
-}
-// D(16x8, fp32) = A(16x16, bf16, row) * B(16x8, bf16, col): the first link of an accumulator chain
-__device__ __forceinline__ void mma_first(float &d0, float &d1, float &d2, float &d3, uint32_t a0, uint32_t a1, uint32_t a2,
-                                          uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d0), "=f"(d1), "=f"(d2), "=f"(d3)
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-}
-
-// Byte offset, inside a staged K or V tile (two 2 KB boxes: columns 0..63 and 64..127), of the 16-byte piece
-// `piece` (0..15) of row `row` (0..15): the 128-byte swizzle of the tensor copy XORs the piece index within a
-// 128-byte line with the line index modulo 8 (the boxes start on 1024-byte boundaries).
-__device__ __forceinline__ uint32_t tile_offset(int row, int piece) {
-  return (uint32_t)((piece >> 3) * kHalfBytes + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-}
 
 // keeps a value that was worked out early in a register, so that the work is not redone (later) where it is used
 __device__ __forceinline__ void pin(uint32_t &x) { asm volatile("" : "+r"(x)); }
@@ -879,25 +818,6 @@ static float stream_geometry(int L, int heads, int G, const DeviceInfo &dev, int
     if (best == 0.f || cost < best) { best = cost; *split = s; *per_cta = per; }
   }
   return best;
-}
-
-// cuTensorMapEncodeTiled, looked up through the runtime (the library does not link against the driver)
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeTiledFn encode_tiled_fn() {
-  static std::once_flag once;
-  static EncodeTiledFn fn = nullptr;
-  std::call_once(once, [] {
-    void *f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(f);
-    else
-      (void)cudaGetLastError();
-  });
-  return fn;
 }
 
 // [B, H_kv, L, 128] bf16 through the cache strides, boxes of 16 rows x 64 columns with the 128-byte swizzle;

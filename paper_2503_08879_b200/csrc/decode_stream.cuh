@@ -39,13 +39,6 @@ struct StShared {
 };
 static_assert(kStStages * kStStageBytes >= kMaxGroup * kStHeadStride * 4, "a warp's result fits into its ring");
 
-// transposes an 8x8 matrix of 16-bit elements held by the warp (lane (g, c): row g, columns 2c and 2c + 1)
-__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
-  uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-
 // split > 1 (a power of two): CTA i takes part i % split of head i / split, a cluster is the split CTAs of a head.
 // split = 1: CTA i takes the whole heads [i * per_cta, (i + 1) * per_cta).
 __global__ void __launch_bounds__(kStThreads, 2)
