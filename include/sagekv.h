@@ -385,6 +385,201 @@ int sagekv_score_static(const sagekv_shape *shape, const void *q_last, const voi
                         int64_t n_ctx, int32_t n_init, int32_t n_recent,
                         float *scores, int64_t scores_row_stride, void *stream);
 
+/* ---- The full cache in pages ------------------------------------------------
+ * A server keeps the full cache of a layer in pages of a few tokens that belong
+ * to sequences through a block table.  The calls below fill such a cache, attend
+ * to it, and run the method's Steps 2 and 3 on it.  The paper keeps one
+ * contiguous cache (Section 2); the layout changes no result.
+ *
+ * Token t of sequence s, KV head g lies in page p = block_table[s*table_stride +
+ * t / page_size], slot t % page_size, at element
+ *     p*page_stride + g*head_stride + (t % page_size)*token_stride
+ * of k_pages and of v_pages, 128 contiguous elements.  Both pools have the same
+ * layout; sequences may share pages.
+ *   dtype      SAGEKV_CACHE_BF16, or SAGEKV_CACHE_E4M3: 8-bit elements that stand
+ *              for code * scale, one fp32 scale per KV head in k_scale / v_scale
+ *              (device, [H_kv]; NULL: 1).  Scales must be positive and finite.
+ *              NULL for a bf16 cache.
+ *   page_size  tokens per page, a multiple of 16.
+ *   strides    in elements, multiples of 16 bytes, each at least 128 elements.
+ *   n_seqs     sequences in use, at most the context's batch.
+ *   seq_lens   int32 [n_seqs], tokens in each sequence (0 is allowed); read by
+ *              sagekv_paged_attn alone, may be NULL for the other calls.
+ * block_table and seq_lens are device memory, read by the kernels: a captured
+ * launch sees what they hold when it is replayed.  The host cannot check them, so the
+ * kernels do, in every build: a page id outside [0, n_pages), a sequence or a
+ * position outside the table, a length beyond max_pages * page_size sets bit 1
+ * of the status word (sagekv_status: SAGEKV_ERR_BOUNDS) and the access is left
+ * out, as each call says.  Errors of every call that takes one (see
+ * sagekv_paged_check): INVALID (null, sizes or strides too small, an unknown
+ * dtype), ALIGN, UNSUPPORTED (page_size % 16, n_seqs above the batch,
+ * max_pages * page_size above 2^30, n_seqs * H_kv * max_pages * page_size / 16
+ * above 2^31 - 1, page_stride of 2^40 bytes or more). */
+enum { SAGEKV_CACHE_BF16 = 0, SAGEKV_CACHE_E4M3 = 1 };
+
+typedef struct {
+  void *k_pages, *v_pages;
+  int64_t page_stride, head_stride, token_stride;
+  const int32_t *block_table;
+  int64_t table_stride;
+  const int32_t *seq_lens;
+  const float *k_scale, *v_scale;
+  int32_t n_pages, page_size, max_pages, n_seqs, dtype;
+} sagekv_paged_cache;
+
+/* Rows of a tensor [tokens, heads, 128] whose last dimension is contiguous:
+ * strides in elements, multiples of 8, base 16-byte aligned. */
+typedef struct {
+  int64_t token_stride, head_stride;
+} sagekv_rows;
+
+/* What the calls say of this cache description and shape: SAGEKV_OK or the error
+ * they return.  Host-only, needs no device. */
+int sagekv_paged_check(const sagekv_shape *shape, const sagekv_paged_cache *cache);
+
+/* Element offset (see above) of a row in the pools, for the page id that the
+ * table holds for it: what the kernels address.  Host-only.  Negative: INVALID
+ * (null, position < 0 or above 2^31 - 1, page outside [0, n_pages), head < 0,
+ * page_size no multiple of 16). */
+int64_t sagekv_paged_offset(const sagekv_paged_cache *cache, int32_t page, int32_t head, int64_t position);
+
+/* Rotary positions.  The first rotary_dim dimensions of a row turn in pairs,
+ * pair i by the angle position * f_i; the others stay.  With a = amplitude:
+ *     y[u] = a (x[u] cos - x[w] sin),   y[w] = a (x[w] cos + x[u] sin),
+ * pair i = (u, w) = (i, i + rotary_dim/2), or (2i, 2i + 1) if interleaved.
+ * rotary_dim is a multiple of 16, at most 128.  A plan is a plain host struct,
+ * filled by one of the two calls below and read by each call it is passed to;
+ * `turns` holds f_i / (2 pi) as a fraction of 2^64, so that the angle modulo a
+ * revolution is exact for every position (the products and sums are fp32, the
+ * result is rounded once). */
+typedef struct {
+  int32_t rotary_dim, interleaved;
+  float amplitude;
+  int32_t reserved;
+  uint64_t turns[64];
+} sagekv_rope_plan;
+
+/* How the frequencies f_i = theta^(-2i/rotary_dim) are changed for contexts
+ * longer than those a model was trained on:
+ *   LINEAR  f_i / factor (positions interpolated).
+ *   BASE    theta * factor^(r/(r-2)) in the place of theta, r = rotary_dim.
+ *   BANDS   with w_i = original_ctx * f_i / (2 pi), the revolutions within the
+ *           original context: f_i where w_i >= high, f_i / factor where w_i <= low,
+ *           in between the blend s f_i + (1-s) f_i / factor, s = (w_i-low)/(high-low).
+ *   YARN    with d(b) = r ln(original_ctx / (2 pi b)) / (2 ln theta),
+ *           lo = max(floor d(high), 0), hi = min(ceil d(low), r-1) (lo + 0.001 if
+ *           equal), ramp = clamp((i-lo)/(hi-lo), 0, 1):
+ *           ramp f_i / factor + (1-ramp) f_i, and amplitude 0.1 ln(factor) + 1
+ *           (unless `amplitude` is positive, which then is taken).
+ * amplitude: 0 for the rule's own (1 for all but YARN). */
+enum { SAGEKV_ROPE_NONE = 0, SAGEKV_ROPE_LINEAR = 1, SAGEKV_ROPE_BASE = 2, SAGEKV_ROPE_BANDS = 3, SAGEKV_ROPE_YARN = 4 };
+
+typedef struct {
+  int32_t kind;
+  int32_t reserved;
+  double factor, low, high, original_ctx, amplitude;
+} sagekv_rope_scaling;
+
+/* Fill a plan: from a base and a scaling rule (NULL: none), or from the
+ * rotary_dim/2 frequencies themselves (radians per position).  inv_freq, if not
+ * NULL, receives the frequencies that were taken.  Host-only.  Errors: INVALID (null,
+ * theta <= 1, factor < 1 for a scaling, low >= high for BANDS and YARN, values not
+ * finite, a negative frequency or amplitude), UNSUPPORTED (rotary_dim not a
+ * multiple of 16 within 16..128). */
+int sagekv_rope_plan_init(sagekv_rope_plan *plan, int32_t rotary_dim, int32_t interleaved, double theta,
+                          const sagekv_rope_scaling *scaling, double *inv_freq);
+int sagekv_rope_plan_from(sagekv_rope_plan *plan, int32_t rotary_dim, int32_t interleaved, const double *inv_freq,
+                          float amplitude);
+
+/* Rotate rows: out[t, h] = x[t, h] rotated by positions[t].
+ *   x, out     bf16 [n_tokens, n_heads, 128] through xs and os; out may be x
+ *              (with the same strides), other overlaps are undefined.
+ *   positions  int32 [n_tokens], device.  A negative position turns backwards:
+ *              with positions negated the call gives the gradient with respect
+ *              to x of the call with the positions as they are.
+ * n_heads need not be one of the context's head counts.  n_tokens or n_heads 0
+ * launches nothing.  Errors: INVALID (null, negative sizes, strides below 128 where
+ * there is more than one token or head, a plan that no call filled), ALIGN,
+ * UNSUPPORTED (n_tokens above 2^31 - 1), DEVICE, CUDA. */
+int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sagekv_rows xs, int64_t n_tokens,
+                int32_t n_heads, const int32_t *positions, void *out, sagekv_rows os, void *stream);
+
+/* Append: the keys and values of n_tokens new tokens into their pages.
+ *   k, v       bf16 [n_tokens, H_kv, 128], both through kvs.
+ *   positions  int32 [n_tokens], device: the token's place in its sequence.  A
+ *              negative position marks a place without a token (padding): nothing
+ *              is read or written for it.
+ *   seqs       int32 [n_tokens], device: the token's sequence; NULL: token t is
+ *              sequence t's (one new token per sequence).
+ *   plan       keys are rotated by their positions before they are stored; NULL:
+ *              stored as given.  Values are stored as given.
+ *   q, q_out   bf16 [n_tokens, H_q, 128] through qs and qos, or both NULL: the
+ *              tokens' queries, rotated beside in the same launch; q_out may
+ *              be q (with the same strides).
+ * Into a bf16 cache the (rotated) rows are rounded once; into an 8-bit cache the
+ * fp32 values times the reciprocal of the scale are rounded once to the nearest e4m3
+ * value, those beyond +-448 (infinities too) to +-448, NaN to NaN.  seq_lens is neither read nor
+ * changed.  No two tokens of a call may have the same sequence and position, or
+ * reach the same row through shared pages: which of them a part of the row
+ * would come from is undefined.  A token whose sequence, position or page id is out of range is not
+ * stored (its query is rotated) and sets the status bit.
+ * Errors: those of the cache, INVALID (null, exactly one of q and q_out,
+ * strides below 128, negative n_tokens, a plan that no call filled), ALIGN, UNSUPPORTED (n_tokens
+ * above 2^31 - 1), DEVICE, CUDA. */
+int sagekv_paged_append(sagekv_ctx *ctx, const sagekv_paged_cache *cache, const void *k, const void *v,
+                        sagekv_rows kvs, int64_t n_tokens, const int32_t *positions, const int32_t *seqs,
+                        const sagekv_rope_plan *plan, const void *q, sagekv_rows qs, void *q_out, sagekv_rows qos,
+                        void *stream);
+
+/* Attention of one new token per sequence over its whole cache (Section 3.1
+ * "Baselines", full attention, at decode): for every sequence s < n_seqs and
+ * query head h, over the seq_lens[s] tokens of KV head h / G,
+ *     out[s,h] = softmax(scale * q[s,h] . K^T) . V.
+ *   q    bf16 [n_seqs, H_q, 128], sequences q_stride elements apart (a multiple
+ *        of 8, at least H_q*128), heads contiguous.
+ *   out  bf16 [n_seqs, H_q, 128] contiguous;  lse  fp32 [n_seqs, H_q] or NULL
+ *        (natural log of the softmax denominator, maximum included).
+ * A sequence without tokens gives zeros and lse = -infinity.  What a page holds behind
+ * a sequence's last token is not looked at (NaN there does no harm).  A negative length counts as 0 and one beyond the
+ * table as the table's; tokens whose page id is out of range are left out; both set the
+ * status bit.  Rows of out and lse behind n_seqs are not touched.  The work is split
+ * over the tokens by the lengths found on the device and joined by log-sum-exp
+ * inside the same launch, in the order of the tokens: the same inputs give the
+ * same bits.  Products and sums are fp32; the softmax weights are rounded to
+ * bf16 (8-bit cache: to f16) before they multiply V.  The context's scratch is
+ * used, as by the other calls: calls on one context must be ordered, captured graphs that
+ * hold them too.
+ * Errors: those of the cache, INVALID (null, seq_lens NULL, q_stride too small), ALIGN,
+ * DEVICE, CUDA. */
+int sagekv_paged_attn(sagekv_ctx *ctx, const void *q, int64_t q_stride, const sagekv_paged_cache *cache, void *out,
+                      float *lse, void *stream);
+
+/* sagekv_score on a paged cache: every sequence has n_ctx tokens, and n_seqs
+ * must be the context's batch.  Same arithmetic, output, hints and errors as
+ * sagekv_score, plus those of the cache (INVALID also for n_seqs != batch or n_ctx above
+ * max_pages * page_size).  From an 8-bit cache the scores are those of the values it
+ * stands for.  Tokens whose page id is out of range get the score 0 and set the
+ * status bit. */
+int sagekv_paged_score(sagekv_ctx *ctx, const void *q_last, const sagekv_paged_cache *cache, int64_t n_ctx,
+                       int32_t n_init, int32_t n_recent, float *scores, int64_t scores_row_stride, void *stream);
+
+/* Step 3 on a paged cache: the reduced cache that sagekv_select_compact builds,
+ * from lists that sagekv_select_topk has written.
+ *   idx     int32 [batch, H_q, k_q] contiguous, k_q = min(k/G, E): offsets into
+ *           the eviction region (0 is token n_init), as sagekv_select_topk leaves
+ *           them for the rows of sagekv_paged_score.  The lists are taken as they are: order and
+ *           repetitions are kept.  May be NULL if k_q is 0.
+ *   Kc, Vc, cs, state   as for sagekv_select_compact; rows of a bf16 cache are
+ *           bit-exact copies, those of an 8-bit cache code * scale rounded to bf16.
+ * Row r of a list entry or page id out of range is left as it was and sets the
+ * status bit.  Every sequence has n_ctx tokens, n_seqs must be the batch.
+ * Errors: those of the cache, INVALID (null, bad partition, k < 0, k % G != 0,
+ * n_seqs != batch, n_ctx above max_pages * page_size), ALIGN, UNSUPPORTED (n_ctx above max_ctx, L above
+ * max_len, group mode 1), DEVICE, CUDA. */
+int sagekv_paged_compact(sagekv_ctx *ctx, const int32_t *idx, const sagekv_paged_cache *cache, int64_t n_ctx,
+                         int32_t n_init, int32_t n_recent, int32_t k, void *Kc, void *Vc, sagekv_strides cs,
+                         sagekv_cache_state *state, void *stream);
+
 /* Text for a return code; never NULL.  Static storage. */
 const char *sagekv_strerror(int code);
 

@@ -47,7 +47,64 @@ class CacheState(C.Structure):
                 ("ring_len", C.c_int32), ("len", C.c_int32), ("d_step", C.c_void_p)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RopePlan(C.Structure):
+    """Rotary positions as the kernels take them (sagekv_rope_plan); made by sagekv_rope_plan or sagekv_rope_plan_from."""
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32),
+                ("turns", C.c_uint64 * 64)]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("original_ctx", C.c_double), ("amplitude", C.c_double)]
+
+
+ROPE_KINDS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "yarn": 4}
+CACHE_BF16, CACHE_E4M3 = 0, 1
+
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
+
+
+class PagedCache(C.Structure):
+    """One layer's full cache in pages: the C struct sagekv_paged_cache, and the tensors that it points to.
+
+      k_pages, v_pages   [n_pages, H_kv, page_size, 128], torch.bfloat16 or torch.float8_e4m3fn, last dimension contiguous, the same
+                         strides (other orders of the first three dimensions by a permuted view)
+      block_table        int32 [n_seqs, max_pages], last dimension contiguous
+      seq_lens           int32 [n_seqs], contiguous; wanted by paged_attn alone
+      k_scale, v_scale   fp32 [H_kv], contiguous; 8-bit caches, value = code * scale (None: 1)
+    """
+    _fields_ = [("k_pages", _vp), ("v_pages", _vp), ("page_stride", _i64), ("head_stride", _i64), ("token_stride", _i64),
+                ("block_table", _vp), ("table_stride", _i64), ("seq_lens", _vp), ("k_scale", _vp), ("v_scale", _vp),
+                ("n_pages", _i32), ("page_size", _i32), ("max_pages", _i32), ("n_seqs", _i32), ("dtype", _i32)]
+
+    def __init__(self, k_pages, v_pages, block_table, seq_lens=None, k_scale=None, v_scale=None):
+        if k_pages.dim() != 4 or k_pages.stride(3) != 1 or k_pages.shape[3] != 128:
+            raise ValueError("expected pages [n_pages, H_kv, page_size, 128] with contiguous last dimension")
+        if v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype:
+            raise ValueError("expected v_pages with the shape, the strides and the type of k_pages")
+        if k_pages.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError("expected pages of torch.bfloat16 or torch.float8_e4m3fn")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+            raise ValueError("expected an int32 block table [n_seqs, max_pages] with contiguous rows")
+        n_seqs, max_pages = block_table.shape
+        if seq_lens is not None and (seq_lens.dtype != torch.int32 or tuple(seq_lens.shape) != (n_seqs,) or not seq_lens.is_contiguous()):
+            raise ValueError("expected contiguous int32 seq_lens, one per row of the block table")
+        for s in (k_scale, v_scale):
+            if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (k_pages.shape[1],) or not s.is_contiguous()):
+                raise ValueError("expected contiguous float32 scales, one per KV head")
+        self.tensors = (k_pages, v_pages, block_table, seq_lens, k_scale, v_scale)
+        if any(t is not None and t.device != k_pages.device for t in self.tensors):
+            raise ValueError("expected all tensors of a cache on one device")
+        ptr = lambda t: None if t is None else t.data_ptr()
+        super().__init__(ptr(k_pages), ptr(v_pages), k_pages.stride(0), k_pages.stride(1), k_pages.stride(2), ptr(block_table),
+                         max(block_table.stride(0), max_pages), ptr(seq_lens), ptr(k_scale), ptr(v_scale), k_pages.shape[0],
+                         k_pages.shape[2], max_pages, n_seqs, CACHE_BF16 if k_pages.dtype == torch.bfloat16 else CACHE_E4M3)
+
+
 lib.sagekv_create.argtypes = [C.POINTER(_vp), C.POINTER(Shape), _i64, _i32]
 lib.sagekv_destroy.argtypes = [_vp]
 lib.sagekv_budget_split.argtypes = [_i32, _i32, C.POINTER(_i32), C.POINTER(_i32), C.POINTER(_i32)]
@@ -80,6 +137,24 @@ lib.sagekv_quest_bounds.argtypes = [_vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]
 lib.sagekv_quest_bounds.restype = C.c_int
 lib.sagekv_select_topk.argtypes = [_vp, _vp, _i64, _i64, _i32, _vp, _vp]
 lib.sagekv_select_topk.restype = C.c_int
+lib.sagekv_paged_check.argtypes = [C.POINTER(Shape), C.POINTER(PagedCache)]
+lib.sagekv_paged_check.restype = C.c_int
+lib.sagekv_paged_offset.argtypes = [C.POINTER(PagedCache), _i32, _i32, _i64]
+lib.sagekv_paged_offset.restype = _i64
+lib.sagekv_rope_plan_init.argtypes = [C.POINTER(RopePlan), _i32, _i32, C.c_double, C.POINTER(RopeScaling), C.POINTER(C.c_double)]
+lib.sagekv_rope_plan_init.restype = C.c_int
+lib.sagekv_rope_plan_from.argtypes = [C.POINTER(RopePlan), _i32, _i32, C.POINTER(C.c_double), C.c_float]
+lib.sagekv_rope_plan_from.restype = C.c_int
+lib.sagekv_rope.argtypes = [_vp, C.POINTER(RopePlan), _vp, Rows, _i64, _i32, _vp, _vp, Rows, _vp]
+lib.sagekv_rope.restype = C.c_int
+lib.sagekv_paged_append.argtypes = [_vp, C.POINTER(PagedCache), _vp, _vp, Rows, _i64, _vp, _vp, C.POINTER(RopePlan), _vp, Rows, _vp, Rows, _vp]
+lib.sagekv_paged_append.restype = C.c_int
+lib.sagekv_paged_attn.argtypes = [_vp, _vp, _i64, C.POINTER(PagedCache), _vp, _vp, _vp]
+lib.sagekv_paged_attn.restype = C.c_int
+lib.sagekv_paged_score.argtypes = [_vp, _vp, C.POINTER(PagedCache), _i64, _i32, _i32, _vp, _i64, _vp]
+lib.sagekv_paged_score.restype = C.c_int
+lib.sagekv_paged_compact.argtypes = [_vp, _vp, C.POINTER(PagedCache), _i64, _i32, _i32, _i32, _vp, _vp, Strides, C.POINTER(CacheState), _vp]
+lib.sagekv_paged_compact.restype = C.c_int
 lib.sagekv_status.argtypes = [_vp, C.POINTER(_i32)]
 lib.sagekv_status.restype = C.c_int
 lib.sagekv_status_code.argtypes = [_i32]
@@ -129,6 +204,10 @@ def _stream():
 _marshal.bind(*(C.cast(f, _vp).value for f in (lib.sagekv_score, lib.sagekv_select_compact, lib.sagekv_decode_attn,
                                                lib.sagekv_pool_scores, lib.sagekv_quest_bounds, lib.sagekv_select_topk)),
               _stream_handle, C.ArgumentError)
+
+
+_marshal.bind_paged(*(C.cast(f, _vp).value for f in (lib.sagekv_rope, lib.sagekv_paged_append, lib.sagekv_paged_attn, lib.sagekv_paged_score,
+                                                     lib.sagekv_paged_compact)))
 
 
 def _kv_strides(t: torch.Tensor) -> Strides:
@@ -238,6 +317,72 @@ def sagekv_score_static(shape: Shape, q_last, K, n_ctx: int, n_init: int, n_rece
                                    _ptr(scores), scores_row_stride, _stream()), "sagekv_score_static")
 
 
+def sagekv_rope_plan(rotary_dim: int, interleaved: bool, theta: float, scaling: dict = None) -> RopePlan:
+    """A rotary plan from a base and a scaling rule: dict(kind="linear" | "base" | "bands" | "yarn", factor=...,
+    low=..., high=..., original_ctx=..., amplitude=...), the entries its kind takes (None: unscaled)."""
+    plan, rule = RopePlan(), None
+    if scaling is not None:
+        extra = set(scaling) - {"kind", "factor", "low", "high", "original_ctx", "amplitude"}
+        if extra or scaling.get("kind") not in ROPE_KINDS:
+            raise ValueError("unknown scaling rule: %r" % (scaling,))
+        rule = RopeScaling(ROPE_KINDS[scaling["kind"]], 0, scaling.get("factor", 1.0), scaling.get("low", 0.0), scaling.get("high", 0.0),
+                           scaling.get("original_ctx", 0.0), scaling.get("amplitude", 0.0))
+    _check(lib.sagekv_rope_plan_init(C.byref(plan), rotary_dim, bool(interleaved), theta, None if rule is None else C.byref(rule), None),
+           "sagekv_rope_plan_init")
+    return plan
+
+
+def sagekv_rope_plan_from(rotary_dim: int, interleaved: bool, inv_freq, amplitude: float = 1.0) -> RopePlan:
+    """A rotary plan from rotary_dim / 2 frequencies in radians per position."""
+    f = [float(x) for x in inv_freq]
+    if len(f) != rotary_dim // 2:
+        raise ValueError("expected rotary_dim / 2 frequencies")
+    plan = RopePlan()
+    _check(lib.sagekv_rope_plan_from(C.byref(plan), rotary_dim, bool(interleaved), (C.c_double * len(f))(*f), amplitude), "sagekv_rope_plan_from")
+    return plan
+
+
+def sagekv_paged_check(shape: Shape, cache: PagedCache):
+    _check(lib.sagekv_paged_check(C.byref(shape), C.byref(cache)), "sagekv_paged_check")
+
+
+def sagekv_paged_offset(cache: PagedCache, page: int, head: int, position: int) -> int:
+    at = lib.sagekv_paged_offset(C.byref(cache), page, head, position)
+    if at < 0:
+        _check(int(at), "sagekv_paged_offset")
+    return int(at)
+
+
+def sagekv_rope(ctx, plan: RopePlan, x, n_tokens: int, n_heads: int, positions, out):
+    code = _marshal.rope(ctx, plan, x, n_tokens, n_heads, positions, out)
+    if code:
+        _check(code, "sagekv_rope", ctx)
+
+
+def sagekv_paged_append(ctx, cache: PagedCache, k, v, n_tokens: int, positions, seqs=None, plan: RopePlan = None, q=None, q_out=None):
+    code = _marshal.paged_append(ctx, cache, k, v, n_tokens, positions, seqs, plan, q, q_out)
+    if code:
+        _check(code, "sagekv_paged_append", ctx)
+
+
+def sagekv_paged_attn(ctx, q, cache: PagedCache, out, lse=None):
+    code = _marshal.paged_attn(ctx, q, cache, out, lse)
+    if code:
+        _check(code, "sagekv_paged_attn", ctx)
+
+
+def sagekv_paged_score(ctx, q_last, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, scores, scores_row_stride: int):
+    code = _marshal.paged_score(ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores_row_stride)
+    if code:
+        _check(code, "sagekv_paged_score", ctx)
+
+
+def sagekv_paged_compact(ctx, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, Kc, Vc, state: CacheState):
+    code = _marshal.paged_compact(ctx, idx, cache, n_ctx, n_init, n_recent, k, Kc, Vc, state)
+    if code:
+        _check(code, "sagekv_paged_compact", ctx)
+
+
 def sagekv_select_compact(ctx, scores, scores_row_stride: int, K, V, n_ctx: int, n_init: int, n_recent: int, k: int,
                           idx, Kc, Vc, state: CacheState):
     code = _marshal.select_compact(ctx, scores, scores_row_stride, K, V, n_ctx, n_init, n_recent, k, idx, Kc, Vc, state)
@@ -342,3 +487,57 @@ class SageKV:
             out = torch.empty_like(q)
         sagekv_decode_attn(self.ctx, q, k_new, v_new, layer.Kc, layer.Vc, layer.state, out, lse)
         return out
+
+    # ---- the full cache in pages ----
+
+    def rope(self, x, positions, plan: RopePlan, out=None):
+        """Rows x [tokens, heads, 128] rotated by their positions (int32 [tokens]); out may be x."""
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if positions.dtype != torch.int32 or positions.shape != x.shape[:1] or out.shape != x.shape:
+            raise ValueError("expected int32 positions, one per token, and out like x")
+        sagekv_rope(self.ctx, plan, x, x.shape[0], x.shape[1], positions, out)
+        return out
+
+    def paged_append(self, cache: PagedCache, k, v, positions, seqs=None, plan: RopePlan = None, q=None, q_out=None):
+        """Keys and values [tokens, H_kv, 128] into their pages, keys (and queries q, into q_out) rotated by the plan.  Without
+        seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
+        n = k.shape[0]
+        if positions.dtype != torch.int32 or positions.shape != (n,) or v.shape != k.shape or k.shape[1:] != (self.shape[1], 128):
+            raise ValueError("expected k and v [tokens, H_kv, 128] and int32 positions, one per token")
+        if seqs is not None and (seqs.dtype != torch.int32 or seqs.shape != (n,)):
+            raise ValueError("expected int32 seqs, one per token")
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if q.shape != (n, self.shape[0], 128) or q_out.shape != q.shape:
+                raise ValueError("expected q and q_out [tokens, H_q, 128]")
+        sagekv_paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
+        return q_out
+
+    def paged_attn(self, q, cache: PagedCache, out=None, lse=None):
+        """Attention of one new token per sequence, q [>= n_seqs, H_q, 128], over its cache."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if q.shape[0] < cache.n_seqs or q.shape[1:] != (self.shape[0], 128) or q.stride(1) != 128 or out.shape[0] < cache.n_seqs or \
+                out.shape[1:] != q.shape[1:] or not out.is_contiguous() or (lse is not None and (lse.numel() < cache.n_seqs * self.shape[0] or not lse.is_contiguous())):
+            raise ValueError("expected q [n_seqs, H_q, 128] with its heads side by side, out like it and contiguous, lse [n_seqs, H_q]")
+        sagekv_paged_attn(self.ctx, q, cache, out, lse)
+        return out
+
+    def paged_score(self, q_last, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, scores=None):
+        """score() on a paged cache whose sequences have n_ctx tokens each."""
+        if scores is None:
+            scores = self.new_scores(n_ctx, n_init, n_recent)
+        sagekv_paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
+        return scores
+
+    def paged_compact(self, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, layer: Layer = None):
+        """The reduced cache from lists of offsets into the eviction region, int32 [B, H_q, k_q], as sagekv_select_topk writes
+        them (layer.idx is not touched)."""
+        if idx is not None and (idx.dtype != torch.int32 or not idx.is_contiguous()):
+            raise ValueError("expected contiguous int32 lists")
+        if layer is None:
+            layer = self.new_layer(n_init, n_recent, k)
+        sagekv_paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)
+        return layer

@@ -3,45 +3,15 @@
 #include <mutex>
 #include <new>
 
-#include "common.cuh"
+#include "context.cuh"
 
 using namespace sagekv;
 
-struct sagekv_ctx {
-  sagekv_shape shape;
-  int G;
-  int64_t max_ctx;
-  int32_t max_len;
-  int device;               // the device the context was created on; every call must find it current
-  const DeviceInfo *dev;    // that device's one-time set-up
-  float scale;
-  float2 *score_partials;   // [B*H_q, ceil(max_ctx / kScoreChunk)]
-  int max_chunks;
-  float *decode_partials;   // [B*H_kv, max_splits (clusters per head), kPartialStride]
-  int max_splits;
-  int32_t *tickets;         // [B*H_kv + 1], zero between launches; the status word and the selection's ready word follow them
-  int32_t *status;          // one int32: kStatus* bits raised by the kernels
-  int last_cuda_error;
-  int overlap;              // 0, 1 or 2: see sagekv_set_overlap
-  int select_overlap;       // 0, 1 or 2: see sagekv_set_select_overlap
-  bool select_ahead;        // the last select call releases its successor before it has waited for its own predecessor
-  int decode_variant;       // 0, 1 or 2: see sagekv_set_decode_variant
-  int hint;                 // 0, 1, 2: see sagekv_set_select_hint
-  int32_t hint_k;
-  int group_mode;           // 0: a selection per query head (the paper's), 1: one per KV head from pooled scores
-};
-
 namespace {
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool strides_ok(const sagekv_strides &s) {
   return s.batch_stride % 8 == 0 && s.head_stride % 8 == 0 && s.token_stride % 8 == 0;
 }
-int cuda_fail(sagekv_ctx *ctx, cudaError_t e) {
-  if (ctx) ctx->last_cuda_error = (int)e;
-  return SAGEKV_ERR_CUDA;
-}
-
 // One-time set-up per device (function attributes, SM count, cluster capacities), done with that device current.
 constexpr int kMaxDevices = 64;
 DeviceInfo g_dev[kMaxDevices];
@@ -56,17 +26,12 @@ cudaError_t device_setup(int dev, const DeviceInfo **out) {
     cudaError_t e = cudaDeviceGetAttribute(&d.n_sm, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = select_compact_setup();
     if (e == cudaSuccess) e = decode_setup(&d);
+    if (e == cudaSuccess) e = paged_attn_setup();
     if (e != cudaSuccess) return e;
     d.ready = true;
   }
   *out = &d;
   return cudaSuccess;
-}
-
-// false: another device is current than the one the context belongs to
-bool on_own_device(const sagekv_ctx *ctx) {
-  int cur = -1;
-  return cudaGetDevice(&cur) == cudaSuccess && cur == ctx->device;
 }
 
 }  // namespace
@@ -117,11 +82,17 @@ int sagekv_create(sagekv_ctx **out, const sagekv_shape *shape, int64_t max_ctx, 
     e = cudaMalloc(&ctx->decode_partials, n_heads * ctx->max_splits * kPartialStride * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&ctx->tickets, (n_heads + 3) * sizeof(int32_t));
   if (e == cudaSuccess) e = cudaMemset(ctx->tickets, 0, (n_heads + 3) * sizeof(int32_t));
+  if (e == cudaSuccess)
+    e = cudaMalloc(&ctx->paged_partials, (size_t)paged_attn_max_ctas(ctx->dev->n_sm) * 2 * kPartialStride * sizeof(float));
+  if (e == cudaSuccess) e = cudaMalloc(&ctx->paged_tickets, n_heads * sizeof(int32_t));
+  if (e == cudaSuccess) e = cudaMemset(ctx->paged_tickets, 0, n_heads * sizeof(int32_t));
   if (e == cudaSuccess) ctx->status = ctx->tickets + n_heads + 1;
   if (e != cudaSuccess) {
     cudaFree(ctx->score_partials);
     cudaFree(ctx->decode_partials);
     cudaFree(ctx->tickets);
+    cudaFree(ctx->paged_partials);
+    cudaFree(ctx->paged_tickets);
     delete ctx;
     cudaGetLastError();
     return e == cudaErrorMemoryAllocation ? SAGEKV_ERR_NOMEM : SAGEKV_ERR_CUDA;
@@ -135,6 +106,8 @@ int sagekv_destroy(sagekv_ctx *ctx) {
   cudaFree(ctx->score_partials);
   cudaFree(ctx->decode_partials);
   cudaFree(ctx->tickets);
+  cudaFree(ctx->paged_partials);
+  cudaFree(ctx->paged_tickets);
   delete ctx;
   return SAGEKV_OK;
 }

@@ -37,6 +37,9 @@ struct ScoreParams {
   int32_t *status = nullptr;   // status word of the context, or null (see kStatus*)
 };
 cudaError_t launch_score(const ScoreParams &p, int n_sm, cudaStream_t stream);
+// its second pass alone, for logits and (max, sum) pairs that another kernel has written (p.sketch_off is set)
+cudaError_t launch_score_normalise(const ScoreParams &p, int n_sm, cudaStream_t stream);
+int64_t score_sketch_offset(const ScoreParams &p);   // what launch_score sets p.sketch_off to
 
 // ---- what the score step can leave behind each row for the select step -----------------------------------
 // A row of E scores is cut into 8 slices of sketch_chunk(E) elements and each slice into 512 groups (16-byte

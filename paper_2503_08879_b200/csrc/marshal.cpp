@@ -20,6 +20,13 @@ typedef int (*DecodeFn)(sagekv_ctx *, const void *, const void *, const void *, 
 typedef int (*PoolFn)(sagekv_ctx *, const float *, int64_t, int64_t, int32_t, int32_t, float *, int64_t, void *);
 typedef int (*BoundsFn)(sagekv_ctx *, const void *, const void *, const void *, int64_t, float *, int64_t, void *);
 typedef int (*TopkFn)(sagekv_ctx *, const float *, int64_t, int64_t, int32_t, int32_t *, void *);
+typedef int (*RopeFn)(sagekv_ctx *, const sagekv_rope_plan *, const void *, sagekv_rows, int64_t, int32_t, const int32_t *, void *, sagekv_rows, void *);
+typedef int (*AppendFn)(sagekv_ctx *, const sagekv_paged_cache *, const void *, const void *, sagekv_rows, int64_t, const int32_t *,
+                        const int32_t *, const sagekv_rope_plan *, const void *, sagekv_rows, void *, sagekv_rows, void *);
+typedef int (*PagedAttnFn)(sagekv_ctx *, const void *, int64_t, const sagekv_paged_cache *, void *, float *, void *);
+typedef int (*PagedScoreFn)(sagekv_ctx *, const void *, const sagekv_paged_cache *, int64_t, int32_t, int32_t, float *, int64_t, void *);
+typedef int (*PagedCompactFn)(sagekv_ctx *, const int32_t *, const sagekv_paged_cache *, int64_t, int32_t, int32_t, int32_t, void *, void *,
+                              sagekv_strides, sagekv_cache_state *, void *);
 
 ScoreFn g_score;
 SelectFn g_select;
@@ -27,6 +34,11 @@ DecodeFn g_decode;
 PoolFn g_pool;
 BoundsFn g_bounds;
 TopkFn g_topk;
+RopeFn g_rope;
+AppendFn g_append;
+PagedAttnFn g_paged_attn;
+PagedScoreFn g_paged_score;
+PagedCompactFn g_paged_compact;
 PyObject *g_stream_of;   // callable: handle of the current stream of the current device, as an integer
 PyObject *g_arg_error;   // ctypes.ArgumentError
 PyObject *g_data_ptr, *g_stride;
@@ -75,6 +87,25 @@ bool strides(PyObject *t, sagekv_strides *out) {
   return true;
 }
 
+// strides of a [tokens, heads, 128] tensor whose last dimension is contiguous; None: zeros
+bool rows(PyObject *t, sagekv_rows *out) {
+  *out = {0, 0};
+  if (t == Py_None) return true;
+  PyObject *v = PyObject_CallMethodNoArgs(t, g_stride);
+  if (v == nullptr) return false;
+  int64_t s[3] = {0, 0, 0};
+  const bool three = PyTuple_Check(v) && PyTuple_GET_SIZE(v) == 3;
+  for (int i = 0; three && i < 3; ++i) s[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(v, i));
+  Py_DECREF(v);
+  if (PyErr_Occurred() != nullptr) return false;
+  if (!three || s[2] != 1) {
+    PyErr_SetString(PyExc_ValueError, "expected a [tokens, heads, head_dim] tensor with contiguous head_dim");
+    return false;
+  }
+  out->token_stride = s[0]; out->head_stride = s[1];
+  return true;
+}
+
 // the context handle: a ctypes c_void_p, an integer or None
 bool context(PyObject *o, sagekv_ctx **out) {
   *out = nullptr;
@@ -107,6 +138,26 @@ struct State {
   }
   ~State() { if (b.obj != nullptr) PyBuffer_Release(&b); }
 };
+
+// a ctypes structure that is read during the call; None: null
+template <typename T>
+struct Given {
+  Py_buffer b{};
+  const T *p = nullptr;
+  bool get(PyObject *o, const char *what) {
+    if (o == Py_None) return true;
+    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) return false;
+    if (b.len != (Py_ssize_t)sizeof(T)) {
+      PyErr_Format(PyExc_TypeError, "expected a %s", what);
+      return false;
+    }
+    p = static_cast<const T *>(b.buf);
+    return true;
+  }
+  ~Given() { if (b.obj != nullptr) PyBuffer_Release(&b); }
+};
+typedef Given<sagekv_paged_cache> Cache;
+typedef Given<sagekv_rope_plan> Plan;
 
 bool current_stream(void **out) {
   PyObject *v = PyObject_CallNoArgs(g_stream_of);
@@ -195,6 +246,77 @@ PyObject *select_topk(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return answer([&] { return g_topk(ctx, static_cast<float *>(scores), stride, len, k_q, static_cast<int32_t *>(idx), stream); });
 }
 
+// ctx, plan, x, n_tokens, n_heads, positions, out
+PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  sagekv_ctx *ctx; void *x, *pos, *out, *stream; sagekv_rows xs, os; int64_t tokens; int32_t heads; Plan plan;
+  if (!count(n, 7) || !context(a[0], &ctx) || !plan.get(a[1], "RopePlan") || !pointer(a[2], &x) || !rows(a[2], &xs) || !integer(a[3], &tokens) ||
+      !integer(a[4], &heads) || !pointer(a[5], &pos) || !pointer(a[6], &out) || !rows(a[6], &os) || !current_stream(&stream))
+    return nullptr;
+  return answer([&] { return g_rope(ctx, plan.p, x, xs, tokens, heads, static_cast<int32_t *>(pos), out, os, stream); });
+}
+
+// ctx, cache, k, v, n_tokens, positions, seqs, plan, q, q_out
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  sagekv_ctx *ctx; void *k, *v, *pos, *seqs, *q, *q_out, *stream; sagekv_rows ks, vs, qs, qos; int64_t tokens; Cache cache; Plan plan;
+  if (!count(n, 10) || !context(a[0], &ctx) || !cache.get(a[1], "PagedCache") || !pointer(a[2], &k) || !rows(a[2], &ks) || !pointer(a[3], &v) ||
+      !rows(a[3], &vs) || !integer(a[4], &tokens) || !pointer(a[5], &pos) || !pointer(a[6], &seqs) || !plan.get(a[7], "RopePlan") ||
+      !pointer(a[8], &q) || !rows(a[8], &qs) || !pointer(a[9], &q_out) || !rows(a[9], &qos) || !current_stream(&stream))
+    return nullptr;
+  if (ks.token_stride != vs.token_stride || ks.head_stride != vs.head_stride) {
+    PyErr_SetString(PyExc_ValueError, "expected k and v with the same strides");
+    return nullptr;
+  }
+  return answer([&] {
+    return g_append(ctx, cache.p, k, v, ks, tokens, static_cast<int32_t *>(pos), static_cast<int32_t *>(seqs), plan.p, q, qs, q_out, qos, stream);
+  });
+}
+
+// ctx, q, cache, out, lse
+PyObject *paged_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  sagekv_ctx *ctx; void *q, *out, *lse, *stream; sagekv_rows qs; Cache cache;
+  if (!count(n, 5) || !context(a[0], &ctx) || !pointer(a[1], &q) || !rows(a[1], &qs) || !cache.get(a[2], "PagedCache") || !pointer(a[3], &out) ||
+      !pointer(a[4], &lse) || !current_stream(&stream))
+    return nullptr;
+  return answer([&] { return g_paged_attn(ctx, q, qs.token_stride, cache.p, out, static_cast<float *>(lse), stream); });
+}
+
+// ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores_row_stride
+PyObject *paged_score(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  sagekv_ctx *ctx; void *q, *scores, *stream; int64_t n_ctx, stride; int32_t n_init, n_recent; Cache cache;
+  if (!count(n, 8) || !context(a[0], &ctx) || !pointer(a[1], &q) || !cache.get(a[2], "PagedCache") || !integer(a[3], &n_ctx) ||
+      !integer(a[4], &n_init) || !integer(a[5], &n_recent) || !pointer(a[6], &scores) || !integer(a[7], &stride) || !current_stream(&stream))
+    return nullptr;
+  return answer([&] { return g_paged_score(ctx, q, cache.p, n_ctx, n_init, n_recent, static_cast<float *>(scores), stride, stream); });
+}
+
+// ctx, idx, cache, n_ctx, n_init, n_recent, k, Kc, Vc, state
+PyObject *paged_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  sagekv_ctx *ctx; void *idx, *Kc, *Vc, *stream; sagekv_strides cs; int64_t n_ctx; int32_t n_init, n_recent, k; Cache cache; State st;
+  if (!count(n, 10) || !context(a[0], &ctx) || !pointer(a[1], &idx) || !cache.get(a[2], "PagedCache") || !integer(a[3], &n_ctx) ||
+      !integer(a[4], &n_init) || !integer(a[5], &n_recent) || !integer(a[6], &k) || !pointer(a[7], &Kc) || !strides(a[7], &cs) ||
+      !pointer(a[8], &Vc) || !st.get(a[9]) || !current_stream(&stream))
+    return nullptr;
+  return answer([&] {
+    return g_paged_compact(ctx, static_cast<int32_t *>(idx), cache.p, n_ctx, n_init, n_recent, k, Kc, Vc, cs, st.p, stream);
+  });
+}
+
+// addresses of the paged cache's entry points (rope, paged_append, paged_attn, paged_score, paged_compact)
+PyObject *bind_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!count(n, 5)) return nullptr;
+  void *f[5];
+  for (int i = 0; i < 5; ++i) {
+    f[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred() != nullptr) return nullptr;
+  }
+  g_rope = reinterpret_cast<RopeFn>(f[0]);
+  g_append = reinterpret_cast<AppendFn>(f[1]);
+  g_paged_attn = reinterpret_cast<PagedAttnFn>(f[2]);
+  g_paged_score = reinterpret_cast<PagedScoreFn>(f[3]);
+  g_paged_compact = reinterpret_cast<PagedCompactFn>(f[4]);
+  Py_RETURN_NONE;
+}
+
 // addresses of the six entry points (score, select_compact, decode_attn, pool_scores, quest_bounds, select_topk), the
 // callable that tells the current stream, ctypes.ArgumentError
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -221,6 +343,12 @@ PyCFunction fast(PyObject *(*f)(PyObject *, PyObject *const *, Py_ssize_t)) {
 
 PyMethodDef g_methods[] = {
     {"bind", fast(bind), METH_FASTCALL, nullptr},
+    {"bind_paged", fast(bind_paged), METH_FASTCALL, nullptr},
+    {"rope", fast(rope), METH_FASTCALL, nullptr},
+    {"paged_append", fast(paged_append), METH_FASTCALL, nullptr},
+    {"paged_attn", fast(paged_attn), METH_FASTCALL, nullptr},
+    {"paged_score", fast(paged_score), METH_FASTCALL, nullptr},
+    {"paged_compact", fast(paged_compact), METH_FASTCALL, nullptr},
     {"score", fast(score), METH_FASTCALL, nullptr},
     {"select_compact", fast(select_compact), METH_FASTCALL, nullptr},
     {"decode_attn", fast(decode_attn), METH_FASTCALL, nullptr},

@@ -255,15 +255,24 @@ __global__ void __launch_bounds__(kSketchThreads) score_finalize_sketch_kernel(c
   }
 }
 
+// where the histogram goes, if one is wanted and a row has room for it
+static bool wants_list(const ScoreParams &p) { return p.list_k_q > 0 && list_applies(p.E, p.list_k_q, p.row_stride); }
+
+int64_t score_sketch_offset(const ScoreParams &p) {
+  return !wants_list(p) && p.sketch && sketch_fits(p.E, p.row_stride) ? sketch_offset(p.E) : (int64_t)-1;
+}
+
 cudaError_t launch_score(const ScoreParams &p_in, int n_sm, cudaStream_t stream) {
   if (p_in.E <= 0) return cudaSuccess;
   ScoreParams p = p_in;
-  const bool list = p.list_k_q > 0 && list_applies(p.E, p.list_k_q, p.row_stride);
-  p.sketch_off = !list && p.sketch && sketch_fits(p.E, p.row_stride) ? sketch_offset(p.E) : (int64_t)-1;
+  p.sketch_off = score_sketch_offset(p);
   dim3 grid(p.n_chunks, p.H_kv, p.B);
   cudaError_t err = launch_next(score_logits_kernel, grid, kScoreWarps * 32, 0, stream, 0, p);
-  if (err != cudaSuccess) return err;
-  if (list) return launch_score_finalize_candidates(p, stream);
+  return err != cudaSuccess ? err : launch_score_normalise(p, n_sm, stream);
+}
+
+cudaError_t launch_score_normalise(const ScoreParams &p, int n_sm, cudaStream_t stream) {
+  if (wants_list(p)) return launch_score_finalize_candidates(p, stream);
   const int rows = p.B * p.H_q;
   if (p.sketch_off >= 0)
     return launch_next(score_finalize_sketch_kernel, dim3(kSketchSlices, rows), kSketchThreads, 0, stream, 0, p, sketch_chunk(p.E));
