@@ -508,7 +508,7 @@ int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sa
  *   k, v       bf16 [n_tokens, H_kv, 128], both through kvs.
  *   positions  int32 [n_tokens], device: the token's place in its sequence.  A
  *              negative position marks a place without a token (padding): nothing
- *              is read or written for it.
+ *              is written for it.
  *   seqs       int32 [n_tokens], device: the token's sequence; NULL: token t is
  *              sequence t's (one new token per sequence).
  *   plan       keys are rotated by their positions before they are stored; NULL:
@@ -555,8 +555,8 @@ int sagekv_paged_attn(sagekv_ctx *ctx, const void *q, int64_t q_stride, const sa
                       float *lse, void *stream);
 
 /* sagekv_score on a paged cache: every sequence has n_ctx tokens, and n_seqs
- * must be the context's batch.  Same arithmetic, output, hints and errors as
- * sagekv_score, plus those of the cache (INVALID also for n_seqs != batch or n_ctx above
+ * must be the context's batch.  Same output (the sums of a product in another
+ * order), hints and errors as sagekv_score, plus those of the cache (INVALID also for n_seqs != batch or n_ctx above
  * max_pages * page_size).  From an 8-bit cache the scores are those of the values it
  * stands for.  Tokens whose page id is out of range get the score 0 and set the
  * status bit. */

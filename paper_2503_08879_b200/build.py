@@ -17,7 +17,7 @@ LIB_CHECKED = os.path.join(HERE, "libsagekv_checked.so")   # the same interface 
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 LIB_TRACE = os.path.join(HERE, "libsagekv_trace.so")       # built with -DSAGEKV_TRACE: timeline stamps in the decode kernel
 SOURCES = ["api.cu", "score.cu", "score_static.cu", "select_compact.cu", "decode_attn.cu", "variants.cu", "paged_api.cu", "paged_attn.cu",
-           "paged_cache.cu"]
+           "paged_cache.cu", "paged_score.cu"]
 
 
 def nvcc_path() -> str:

@@ -27,6 +27,7 @@ cudaError_t device_setup(int dev, const DeviceInfo **out) {
     if (e == cudaSuccess) e = select_compact_setup();
     if (e == cudaSuccess) e = decode_setup(&d);
     if (e == cudaSuccess) e = paged_attn_setup();
+    if (e == cudaSuccess) e = paged_score_setup();
     if (e != cudaSuccess) return e;
     d.ready = true;
   }

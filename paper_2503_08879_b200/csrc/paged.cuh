@@ -1,5 +1,5 @@
 // The paged cache inside the library: what a kernel needs to find a token's rows, the arguments of the kernels that
-// work on pages (paged_attn.cu, paged_cache.cu), and conversions from the 8-bit type.
+// work on pages (paged_attn.cu, paged_score.cu, paged_cache.cu), and conversions from the 8-bit type.
 #pragma once
 
 #include "common.cuh"
@@ -83,8 +83,9 @@ struct PagedAppendParams {
 };
 cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm, cudaStream_t stream);
 
-// p.K and p.ks are unused; p.n_chunks is set here
-cudaError_t launch_paged_score(ScoreParams p, const PagedView &c, int dtype, int n_sm, cudaStream_t stream);
+// p.K and p.ks are unused; p.n_chunks (at most max_chunks) is set here
+cudaError_t launch_paged_score(ScoreParams p, const PagedView &c, int dtype, int max_chunks, int n_sm, cudaStream_t stream);
+cudaError_t paged_score_setup();   // one-time function attributes, with the device current
 
 struct PagedCompactParams {
   PagedView c;

@@ -260,7 +260,7 @@ int sagekv_paged_score(sagekv_ctx *ctx, const void *q_last, const sagekv_paged_c
   p.H_kv = ctx->shape.n_kv_heads;
   p.B = ctx->shape.batch;
   p.scale_log2 = ctx->scale * kLog2e;
-  return done(ctx, launch_paged_score(p, view_of(ctx, cache), cache->dtype, ctx->dev->n_sm, static_cast<cudaStream_t>(stream)));
+  return done(ctx, launch_paged_score(p, view_of(ctx, cache), cache->dtype, ctx->max_chunks, ctx->dev->n_sm, static_cast<cudaStream_t>(stream)));
 }
 
 int sagekv_paged_compact(sagekv_ctx *ctx, const int32_t *idx, const sagekv_paged_cache *cache, int64_t n_ctx, int32_t n_init, int32_t n_recent,

@@ -20,38 +20,29 @@
 //
 // A tile's rows behind the sequence's end hold anything: their scores are replaced, not added to, and their V rows are
 // cleared in the fragments, since zero times NaN is NaN.
-#include "paged.cuh"
-#include "tiles.cuh"
+#include "paged_tiles.cuh"
+#include "trace.cuh"
 
 namespace sagekv {
 
-constexpr int kPaWarps = 4;
+constexpr int kPaWarps = 6;
 constexpr int kPaThreads = kPaWarps * 32;
-constexpr int kPaRingBytes = 3 * 2 * kSlotBytes;    // per warp: three stages of bf16 tiles, or six of 8-bit ones
+constexpr int kPaRingBytes = 2 * kSlotBytes;        // per warp: one stage of bf16 tiles, or two of 8-bit ones
 constexpr int kPaHeadStride = kHeadDim + 4;         // floats between the heads of a warp's result: the 32 lanes of a store fall into 32 banks
-constexpr int kPaMinTiles = 4;                      // a CTA's least share of the list: a tile per warp
-constexpr int kPaMaxStages = 6;
-constexpr int kPaMaxParts = kPaWarps * kPaHeadStride;   // most CTAs that may share a pair: their factors lie in sh.o, kMaxGroup floats each
+constexpr int kPaPairCost = 2;                      // places of the list in front of a pair's units: what a change of pair costs a CTA, in units
+constexpr int kPaMinPlaces = 2;                     // a CTA's least share of the list
+constexpr int kPaMaxStages = 2;
+constexpr int kPaJoin = 16;                         // parts of a shared pair that the last CTA reads at once
 
 struct PaShared {
   unsigned char ring[kPaWarps][kPaRingBytes];           // boxes with the 128-byte swizzle: 1024-byte boundaries
   float o[kPaWarps][kMaxGroup * kPaHeadStride];         // results of the warps
   float2 ml[kPaWarps][kMaxGroup];                       // (max, sum) of a warp's tiles
   unsigned long long bar[kPaWarps][kPaMaxStages];
-  int start[4];                                         // where my range begins: sequence, tiles of the list before it, all tiles; arrival order
+  int start[2];                                         // where my range begins (many sequences): sequence, tiles of the list before it
+  int arrived;                                          // parts of a shared pair that had arrived before mine
 };
-static_assert(2 * (sizeof(PaShared) + 1024) <= 228 * 1024, "two CTAs per SM");
-
-__device__ __forceinline__ void tensor_copy_page(uint32_t dst, const CUtensorMap *map, int x, int slot, int head, int page, uint32_t bar,
-                                                 uint64_t policy) {
-  tensor_copy_4d(dst, map, x, slot, head, page, bar, policy);
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
-// byte offset of 16-byte piece `piece` (0..7) of row `row` in a staged tile of 128-byte rows
-__device__ __forceinline__ uint32_t tile8_offset(int row, int piece) { return (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4)); }
+static_assert(kPagedCtasPerSm * (sizeof(PaShared) + 1024) <= 228 * 1024, "they fit on an SM together");
 
 // tokens of a sequence: what the caller gave, cut to what the table can hold
 __device__ __forceinline__ int tokens_of(const PagedView &c, int seq) {
@@ -60,21 +51,38 @@ __device__ __forceinline__ int tokens_of(const PagedView &c, int seq) {
   return len < 0 ? 0 : min(len, most);
 }
 
-// A place in the list of tiles: tile `tile` of head `head` of sequence `seq`, which has `len` tokens.
-struct PaCursor {
-  int seq, head, tile, len;
-  __device__ __forceinline__ int tiles() const { return (len + 15) >> 4; }
-  // moves a tile index that has run past the pair's end on to the pair that holds it
-  __device__ __forceinline__ void settle(const PagedView &c, int H_kv) {
-    while (tile >= tiles() && seq < c.n_seqs) {
-      tile -= tiles();
-      if (len == 0 || ++head == H_kv) {
-        head = 0;
-        len = tokens_of(c, ++seq);
-      }
-    }
+// The lengths of 32 sequences in a row, one per lane of a warp: what moves through the list in order reads memory once
+// per 32 sequences.  All lanes call with the same sequence.
+struct PaLengths {
+  int base, mine;
+  __device__ __forceinline__ void load(const PagedView &c, int seq, int lane) {
+    base = seq;
+    mine = tokens_of(c, seq + lane);
+  }
+  __device__ __forceinline__ int of(const PagedView &c, int seq, int lane) {
+    if (seq - base >= 32) load(c, seq, lane);
+    return __shfl_sync(0xffffffffu, mine, seq - base);
   }
 };
+
+// A place in the list of units: unit `unit` of head `head` of sequence `seq`, which has `len` tokens; `base` is the place of
+// the pair's first unit in the list.
+struct PaCursor {
+  int seq, head, len, unit;
+  uint32_t base;
+  __device__ __forceinline__ int tiles() const { return (len + 15) >> 4; }
+  __device__ __forceinline__ int units() const { return (len + 16 * kPaWarps - 1) / (16 * kPaWarps); }
+  __device__ __forceinline__ void next_pair(const PagedView &c, int H_kv, PaLengths &lens, int lane) {
+    base += (uint32_t)units() + kPaPairCost;
+    unit = 0;
+    if (++head < H_kv) return;
+    head = 0;
+    do len = lens.of(c, ++seq, lane);
+    while (len == 0 && seq < c.n_seqs);
+  }
+};
+// places in the list that the pairs of a sequence take, per head
+__device__ __forceinline__ int places_of(int len) { return len > 0 ? (len + 16 * kPaWarps - 1) / (16 * kPaWarps) + kPaPairCost : 0; }
 
 template <bool kE4m3>
 __global__ void __launch_bounds__(kPaThreads, kPagedCtasPerSm)
@@ -92,6 +100,8 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3, h0 = 2 * c, h1 = 2 * c + 1;
 
+  SAGEKV_TRACE_BEGIN
+  SAGEKV_STAMP(0);
   const uint32_t ring = smem_u32(&sh.ring[warp][0]), bars = smem_u32(&sh.bar[warp][0]);
   if (lane == 0) {
 #pragma unroll
@@ -101,184 +111,187 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
   }
+  __syncwarp();
   wait_for_predecessor();
+  SAGEKV_STAMP(1);
 
-  // ---- my range of the list ----
-  const int per_thread = (p.c.n_seqs + kPaThreads - 1) / kPaThreads;
-  const int s0 = min(tid * per_thread, p.c.n_seqs), s1 = min(s0 + per_thread, p.c.n_seqs);
-  int mine = 0;
-  for (int s = s0; s < s1; ++s) {
-    const int len = p.c.seq_lens[s];
-    if (len < 0 || len > p.c.max_pages * p.c.page_size) atomicOr(p.c.status, kStatusBounds);
-    mine += (tokens_of(p.c, s) + 15) >> 4;
-  }
-  int incl = mine;
+  // ---- my range of the list: [lo, lo + n), which begins in sequence start_seq, start_before tiles from the list's begin ----
+  const int most_tokens = p.c.max_pages * p.c.page_size;
+  const uint32_t n_ctas = gridDim.x;
+  uint32_t total, per_cta, lo;
+  auto cut = [&] {                                           // (all fits 31 bits: the host has checked the most the tables can hold)
+    const uint32_t all = total * (uint32_t)p.H_kv;
+    per_cta = max(all > 0u ? (all - 1u) / n_ctas + 1u : 0u, (uint32_t)kPaMinPlaces);
+    lo = min((uint32_t)blockIdx.x * per_cta, all);
+    return (int)min(per_cta, all - lo);
+  };
+  int n, start_seq = 0, start_before = 0;
+  PaLengths lens;
+  if (p.c.n_seqs <= 32) {                                    // every warp by itself
+    const int given = lane < p.c.n_seqs ? p.c.seq_lens[lane] : 0;
+    if (given < 0 || given > most_tokens) atomicOr(p.c.status, kStatusBounds);
+    lens.base = 0;
+    lens.mine = min(max(given, 0), most_tokens);
+    const int mine = places_of(lens.mine);
+    int incl = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += v;
-  }
-  int *warp_total = reinterpret_cast<int *>(sh.o[0]);
-  if (lane == 31) warp_total[warp] = incl;
-  __syncthreads();
-  int total = 0, before = incl - mine;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    total = (uint32_t)__shfl_sync(0xffffffffu, incl, 31);
+    n = cut();
+    if (n > 0) {
+      start_seq = __ffs(__ballot_sync(0xffffffffu, lo < (uint32_t)incl * p.H_kv)) - 1;
+      start_before = __shfl_sync(0xffffffffu, incl - mine, start_seq) * p.H_kv;
+    }
+  } else {                                                   // a block-wide scan, every thread over some sequences in a row
+    const int per_thread = (p.c.n_seqs + kPaThreads - 1) / kPaThreads;
+    const int s0 = min(tid * per_thread, p.c.n_seqs), s1 = min(s0 + per_thread, p.c.n_seqs);
+    int mine = 0;
+    for (int s = s0; s < s1; ++s) {
+      const int given = p.c.seq_lens[s];
+      if (given < 0 || given > most_tokens) atomicOr(p.c.status, kStatusBounds);
+      mine += places_of(min(max(given, 0), most_tokens));
+    }
+    int incl = mine;
 #pragma unroll
-  for (int w = 0; w < kPaWarps; ++w) {
-    if (w < warp) before += warp_total[w];
-    total += warp_total[w];
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    int *warp_total = reinterpret_cast<int *>(sh.o[0]);
+    if (lane == 31) warp_total[warp] = incl;
+    __syncthreads();
+    int before = incl - mine;
+    total = 0u;
+#pragma unroll
+    for (int w = 0; w < kPaWarps; ++w) {
+      if (w < warp) before += warp_total[w];
+      total += (uint32_t)warp_total[w];
+    }
+    n = cut();
+    if (lo >= (uint32_t)before * p.H_kv && lo < (uint32_t)(before + mine) * p.H_kv) {   // the range begins in one of this thread's sequences
+      int at = before, s = s0;
+      for (int t; at + (t = places_of(tokens_of(p.c, s))) <= (int)(lo / p.H_kv); ++s) at += t;
+      sh.start[0] = s;
+      sh.start[1] = at * p.H_kv;
+    }
+    __syncthreads();
+    if (n > 0) {
+      start_seq = sh.start[0];
+      start_before = sh.start[1];
+    }
+    lens.load(p.c, start_seq, lane);
   }
-  const int n_ctas = (int)gridDim.x;
-  const int all = total * p.H_kv;                            // fits: the host has checked the most the tables can hold
-  int per_cta = max((int)(((int64_t)all + n_ctas - 1) / n_ctas), kPaMinTiles);
-  if (per_cta < 64) per_cta = (per_cta + kPaWarps - 1) & ~(kPaWarps - 1);   // the same for the busiest warp, fewer parts to join
-  const int lo = (int)min((int64_t)blockIdx.x * per_cta, (int64_t)all), n = min(per_cta, all - lo);
-  if (mine > 0 && lo >= before * p.H_kv && lo < (before + mine) * p.H_kv) {   // the range begins in one of this thread's sequences
-    int at = before, s = s0;
-    for (int len; at + (len = (tokens_of(p.c, s) + 15) >> 4) <= lo / p.H_kv; ++s) at += len;
-    sh.start[0] = s;
-    sh.start[1] = at * p.H_kv;
-  }
-  __syncthreads();
 
-  if (n > 0) {
-    // ---- requests: one tile ahead the page id, kStages tiles ahead the rows ----
-    PaCursor next;                                           // my next tile to request
-    next.seq = sh.start[0];
-    next.len = tokens_of(p.c, next.seq);
-    const int into = lo - sh.start[1], first_head = into / next.tiles(), first_tile = into - first_head * next.tiles();
-    next.head = first_head;
-    next.tile = first_tile + warp;
-    int rx = warp;                                           // its index in my range
-    const int tiles_per_page = p.c.page_size >> 4;
-    uint64_t stream_policy;
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(stream_policy));
-    int next_page = -1, next_slot = 0;
-    auto look_up = [&] {
-      next_page = -1;
-      if (rx >= n) return;
-      next.settle(p.c, p.H_kv);
-      if (next.seq >= p.c.n_seqs) return;
-      const int entry = next.tile / tiles_per_page;
-      next_slot = (next.tile - entry * tiles_per_page) << 4;
-      next_page = p.c.table[(int64_t)next.seq * p.c.table_stride + entry];
-    };
-    uint32_t absent = 0u;                                    // stages whose page id is none: nothing is on its way
-    auto request = [&](int s) {
-      if (rx >= n) return;
-      const uint32_t bar = bars + 8u * s;
-      if (next_page >= 0 && next_page < p.c.n_pages) {
-        absent &= ~(1u << s);
-        if (lane == 0) mbar_expect_tx(bar, kStageBytes);
-        __syncwarp();
-        constexpr int kBoxes = kE4m3 ? 2 : 4;                // 16 rows of 128 bytes each
-        if (lane < kBoxes)
-          tensor_copy_page(ring + (uint32_t)(s * kStageBytes + lane * kHalfBytes), lane < kBoxes / 2 ? &map_k : &map_v,
-                           kE4m3 ? 0 : (lane & 1) * 64, next_slot, next.head, next_page, bar, stream_policy);
-      } else {
-        absent |= 1u << s;
-        if (lane == 0) {
-          mbar_arrive(bar);
-          atomicOr(p.c.status, kStatusBounds);
-        }
+  SAGEKV_STAMP_AFTER(2, (float)n);
+
+  // ---- requests ----
+  const uint32_t hi = lo + (uint32_t)max(n, 0);
+  PaCursor begin, next;                                      // where my range begins; my next tile to request
+  PaLengths ahead = lens;
+  bool more = false;                                         // there is one
+  int ids = -1, ids_unit = 0;                                // page ids of the warp's tiles in 32 units of the pair, from ids_unit on
+  int next_page = -1, next_slot = 0;
+  uint32_t absent = 0u;                                      // stages whose page id is none: nothing is on its way
+  uint64_t stream_policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(stream_policy));
+  auto look_up = [&](bool moved) {                           // settles on the next tile, if there is one, and finds its page
+    while (next.unit >= next.units() || next.unit * kPaWarps + warp >= next.tiles()) {   // (a pair's last unit may lack my tile)
+      next.next_pair(p.c, p.H_kv, ahead, lane);
+      moved = true;
+      if (next.base >= hi) break;
+    }
+    more = next.base + (uint32_t)next.unit < hi && next.seq < p.c.n_seqs;
+    if (!more) return;
+    if (moved || next.unit - ids_unit >= 32) {
+      ids_unit = next.unit;
+      const int tile = (next.unit + lane) * kPaWarps + warp;
+      ids = tile < next.tiles() ? p.c.table[(int64_t)next.seq * p.c.table_stride + page_of(tile << 4, p.c.page_size, p.c.page_magic)] : -1;
+    }
+    const int first = (next.unit * kPaWarps + warp) << 4;
+    next_slot = first - page_of(first, p.c.page_size, p.c.page_magic) * p.c.page_size;
+    next_page = __shfl_sync(0xffffffffu, ids, next.unit - ids_unit);
+  };
+  auto request = [&](int s) {
+    if (!more) return;
+    const uint32_t bar = bars + 8u * s;
+    if (next_page >= 0 && next_page < p.c.n_pages) {
+      absent &= ~(1u << s);
+      if (lane == 0) mbar_expect_tx(bar, kStageBytes);
+      __syncwarp();
+      constexpr int kBoxes = kE4m3 ? 2 : 4;                  // 16 rows of 128 bytes each
+      if (lane < kBoxes)
+        tensor_copy_4d(ring + (uint32_t)(s * kStageBytes + lane * kHalfBytes), lane < kBoxes / 2 ? &map_k : &map_v,
+                         kE4m3 ? 0 : (lane & 1) * 64, next_slot, next.head, next_page, bar, stream_policy);
+    } else {
+      absent |= 1u << s;
+      if (lane == 0) {
+        mbar_arrive(bar);
+        atomicOr(p.c.status, kStatusBounds);
       }
-      rx += kPaWarps;
-      next.tile += kPaWarps;
-      look_up();
-    };
-    look_up();
+    }
+    ++next.unit;
+    look_up(false);
+  };
+  if (n > 0) {
+    begin.seq = start_seq;
+    begin.len = ahead.of(p.c, start_seq, lane);
+    const uint32_t into = lo - (uint32_t)start_before, places = (uint32_t)places_of(begin.len);
+    begin.head = (int)(into / places);
+    begin.base = (uint32_t)start_before + (uint32_t)begin.head * places + kPaPairCost;
+    begin.unit = max((int)(lo - begin.base), 0);             // (the range may begin in the places in front of the pair)
+    next = begin;
+    look_up(true);
 #pragma unroll
     for (int s = 0; s < kStages; ++s) request(s);
+  }
+  SAGEKV_STAMP(3);
 
+  // ---- sequences without tokens ----
+  for (int s = blockIdx.x; s < p.c.n_seqs; s += n_ctas) {
+    if ((p.c.n_seqs <= 32 ? __shfl_sync(0xffffffffu, lens.mine, s) : tokens_of(p.c, s)) > 0) continue;
+    for (int i = tid; i < p.H_q * (kHeadDim / 8); i += kPaThreads) st_v4(p.out + (int64_t)s * p.H_q * kHeadDim + i * 8, make_uint4(0u, 0u, 0u, 0u));
+    if (p.lse != nullptr)
+      for (int i = tid; i < p.H_q; i += kPaThreads) p.lse[(int64_t)s * p.H_q + i] = -INFINITY;
+  }
+
+  if (n > 0) {
     // fragment addresses within a stage
     const int mi = lane >> 3, l8 = lane & 7;
     uint32_t k_off[8], v_off[8];
+    k_fragment_offsets<kE4m3>(lane, k_off);
 #pragma unroll
-    for (int j = 0; j < (kE4m3 ? 4 : 8); ++j) {
-      if (kE4m3) {
-        k_off[j] = v_off[j] = tile8_offset((mi & 1) * 8 + l8, 2 * j + (mi >> 1));
-        v_off[j] += kTileBytes;
-      } else {
-        k_off[j] = tile_offset((mi & 1) * 8 + l8, 2 * j + (mi >> 1));
-        v_off[j] = kTileBytes + tile_offset((mi >> 1) * 8 + l8, 2 * j + (mi & 1));
-      }
-    }
+    for (int j = 0; j < (kE4m3 ? 4 : 8); ++j)
+      v_off[j] = kTileBytes + (kE4m3 ? k_off[j] : tile_offset((mi >> 1) * 8 + l8, 2 * j + (mi & 1)));
     const bool in0 = h0 < p.G, in1 = h1 < p.G;
 
     bool timed_out = false;
     int stage = 0;
     uint32_t phase = 0;
-    int x = warp;                                            // my next tile, as an index into my range
-    PaCursor at;                                             // the pair being worked on
-    at.seq = sh.start[0];
-    at.len = tokens_of(p.c, at.seq);
-    at.head = first_head;
-    int pair_x0 = -first_tile;                               // index (may be negative) of the pair's tile 0 in the range
-    while (pair_x0 < n && at.seq < p.c.n_seqs) {
-      const int pair_tiles = at.tiles(), x_end = min(n, pair_x0 + pair_tiles);
-      // B fragments of Q^T: lane (g, c) holds of head g, bf16: dims 16j + 2c, +1 and 16j + 8 + 2c, +1; 8-bit: 16j + 4c .. + 3
+    PaCursor at = begin;                                     // the pair being worked on
+    while (at.base < hi && at.seq < p.c.n_seqs) {
+      const int tiles = at.tiles(), unit_end = min(at.units(), (int)(hi - at.base));
       uint32_t qb[8][2];
-      float mult0 = p.scale_log2, mult1 = p.scale_log2;      // what brings a score of heads 2c, 2c + 1 to log2 units
-      {
-        const uint16_t *q_row = p.q + (int64_t)at.seq * p.q_stride + (at.head * p.G + min(g, p.G - 1)) * kHeadDim;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          qb[j][0] = qb[j][1] = 0u;
-          if (g < p.G) {
-            if (kE4m3) {
-              const uint2 v = *reinterpret_cast<const uint2 *>(q_row + 16 * j + 4 * c);
-              qb[j][0] = v.x; qb[j][1] = v.y;
-            } else {
-              qb[j][0] = *reinterpret_cast<const uint32_t *>(q_row + 16 * j + 2 * c);
-              qb[j][1] = *reinterpret_cast<const uint32_t *>(q_row + 16 * j + 8 + 2 * c);
-            }
-          }
-        }
-        if (kE4m3) {
-          float largest = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) largest = fmaxf(largest, fmaxf(fabsf(bf16_low(qb[j][e])), fabsf(bf16_high(qb[j][e]))));
-          largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
-          largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
-          const int e = query_exponent(largest);
-          const float up = power_of_two(e);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) qb[j][i] = pack_f16x2(bf16_low(qb[j][i]) * up, bf16_high(qb[j][i]) * up);
-          const float base = p.c.k_scale != nullptr ? p.scale_log2 * p.c.k_scale[at.head] : p.scale_log2;
-          mult0 = base * power_of_two(-__shfl_sync(0xffffffffu, e, h0 * 4));
-          mult1 = base * power_of_two(-__shfl_sync(0xffffffffu, e, h1 * 4));
-        }
-      }
+      float mult0, mult1;
+      load_queries<kE4m3>(p.q + (int64_t)at.seq * p.q_stride + at.head * p.G * kHeadDim, p.G, p.c.k_scale, at.head, p.scale_log2, lane, qb, mult0, mult1);
 
       float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // the maxima are kept kWeightShift below the scores'
       float acc[8][4];
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 
-      for (; x < x_end; x += kPaWarps) {
+      for (int tile = at.unit * kPaWarps + warp; tile < min(tiles, unit_end * kPaWarps); tile += kPaWarps) {
         const uint32_t tb = ring + (uint32_t)(stage * kStageBytes);
         if (!mbar_wait(bars + 8u * stage, phase)) timed_out = true;
+        if (at.base + at.unit <= lo + kPaPairCost && tile == at.unit * kPaWarps + warp) SAGEKV_STAMP(4);
         if (!((absent >> stage) & 1u)) {
-          // ---- S = K Q^T, four accumulator chains: lane (g, c) gets tokens g, g + 8 of heads 2c, 2c + 1 ----
-          float ch[4][4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) ch[j][0] = ch[j][1] = ch[j][2] = ch[j][3] = 0.f;
-          uint32_t fa[4];
-          uint32_t va[8][4];
+          // ---- S = K Q^T; V's fragments on their way meanwhile ----
+          float sv[4];
+          score_tile<kE4m3>(tb, k_off, qb, mult0, mult1, sv);
+          uint32_t fa[4], va[8][4];
           if (kE4m3) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              ldmatrix_x4(tb + k_off[j], fa[0], fa[1], fa[2], fa[3]);
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                float(&d)[4] = ch[(2 * j + e) & 3];
-                mma_f16_16816(d[0], d[1], d[2], d[3], f16x2_low(fa[2 * e]), f16x2_low(fa[2 * e + 1]), f16x2_high(fa[2 * e]),
-                              f16x2_high(fa[2 * e + 1]), qb[2 * j + e][0], qb[2 * j + e][1]);
-              }
-            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               // tokens 2c, 2c + 1 (and + 8) of dims 2g, 2g + 1 of two pieces, regrouped by dim
@@ -295,19 +308,10 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
             }
           } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              ldmatrix_x4(tb + k_off[j], fa[0], fa[1], fa[2], fa[3]);
-              float(&d)[4] = ch[j & 3];
-              mma_bf16_16816(d[0], d[1], d[2], d[3], fa[0], fa[1], fa[2], fa[3], qb[j][0], qb[j][1]);
-            }
-#pragma unroll
             for (int j = 0; j < 8; ++j) ldmatrix_x4_trans(tb + v_off[j], va[j][0], va[j][1], va[j][2], va[j][3]);
           }
           // ---- softmax weights ----
-          float sv[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sv[e] = ((ch[0][e] + ch[1][e]) + (ch[2][e] + ch[3][e])) * (e & 1 ? mult1 : mult0);
-          const int left = at.len - ((x - pair_x0) << 4);    // tokens of the sequence from this tile's first on
+          const int left = at.len - (tile << 4);    // tokens of the sequence from this tile's first on
           if (left < 16) {
             if (g >= left) sv[0] = sv[1] = -INFINITY;
             if (g + 8 >= left) sv[2] = sv[3] = -INFINITY;
@@ -350,6 +354,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
 
+      SAGEKV_STAMP_AFTER(5, acc[0][0] + acc[7][3]);
       // ---- the pair (or my part of it) is done: merge the four warps ----
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
@@ -365,8 +370,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         o0[0] = acc[j][0]; o1[0] = acc[j][1]; o0[kStep] = acc[j][2]; o1[kStep] = acc[j][3];
       }
       __syncthreads();
-      const int pair_first = lo + pair_x0;                   // the pair's first tile in the list
-      const int cta_first = pair_first / per_cta, cta_last = (pair_first + pair_tiles - 1) / per_cta;
+      const int cta_first = (int)(at.base / per_cta), cta_last = (int)((at.base + (uint32_t)at.units() - 1u) / per_cta);
       const bool whole = cta_first == cta_last;
       const int64_t row0 = (int64_t)at.seq * p.H_q + at.head * p.G;   // the pair's first row of out and lse
       const float v_scale = kE4m3 && p.c.v_scale != nullptr ? p.c.v_scale[at.head] : 1.f;
@@ -398,85 +402,63 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
           if (col == 0) *reinterpret_cast<float2 *>(part + kMaxGroup * kHeadDim + 2 * h) = make_float2(M, l);
         }
       }
+      SAGEKV_STAMP(6);
       if (!whole) {
-        __threadfence();
-        __syncthreads();
         const int parts = cta_last - cta_first + 1;
         int32_t *ticket = p.tickets + (int64_t)at.seq * p.H_kv + at.head;
-        if (tid == 0) sh.start[3] = atomicAdd(ticket, 1);
         __syncthreads();
-        if (sh.start[3] == parts - 1) {                      // every other part is in scratch
+        if (tid == 0) {
+          __threadfence();                                   // (behind the barrier it stands for the whole block)
+          sh.arrived = atomicAdd(ticket, 1);
           __threadfence();
+        }
+        __syncthreads();
+        SAGEKV_STAMP(7);
+        if (sh.arrived == parts - 1) {                       // every other part is in scratch
           if (tid == 0) *ticket = 0;
           const float *first = p.partials + ((int64_t)cta_first * 2 + 1) * kPartialStride;
-          auto part_of = [&](int i) { return i == 0 ? first : first + ((int64_t)i * 2 - 1) * kPartialStride; };
-          float *factor = sh.o[0];                           // [part][head]; every thread has read the warps' results
-          float Ms[kMaxGroup / 4], ls[kMaxGroup / 4];        // of the heads h = warp, warp + 4: their lanes take the parts in turn
-#pragma unroll
-          for (int k = 0; k < kMaxGroup / 4; ++k) {
-            const int h = warp + 4 * k;
-            Ms[k] = -INFINITY; ls[k] = 0.f;
-            if (h < p.G) {
-              for (int i = lane; i < parts; i += 32) Ms[k] = fmaxf(Ms[k], __ldcg(part_of(i) + kMaxGroup * kHeadDim + 2 * h));
-#pragma unroll
-              for (int o = 1; o < 32; o <<= 1) Ms[k] = fmaxf(Ms[k], __shfl_xor_sync(0xffffffffu, Ms[k], o));
-              for (int i = lane; i < parts; i += 32) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(part_of(i) + kMaxGroup * kHeadDim + 2 * h));
-                const float f = ml.x == Ms[k] ? 1.f : fast_exp2(ml.x - Ms[k]);
-                factor[i * kMaxGroup + h] = f;
-                ls[k] += ml.y * f;
-              }
-#pragma unroll
-              for (int o = 1; o < 32; o <<= 1) ls[k] += __shfl_xor_sync(0xffffffffu, ls[k], o);
-              if (lane == 0) sh.ml[0][h] = make_float2(Ms[k], ls[k]);
-            }
-          }
-          __syncthreads();
           for (int item = tid; item < p.G * (kHeadDim / 4); item += kPaThreads) {
             const int h = item >> 5, col = (item & 31) * 4;
+            float M = -INFINITY, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-            for (int i = 0; i < parts; ++i) {
-              const float4 v = __ldcg(reinterpret_cast<const float4 *>(part_of(i) + h * kHeadDim + col));
-              const float f = factor[i * kMaxGroup + h];
-              o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+            for (int i0 = 0; i0 < parts; i0 += kPaJoin) {    // kPaJoin parts' loads in flight
+              float2 ml[kPaJoin];
+              float4 v[kPaJoin];
+#pragma unroll
+              for (int u = 0; u < kPaJoin; ++u) {
+                const int i = i0 + u;
+                const float *part = i == 0 ? first : first + ((int64_t)i * 2 - 1) * kPartialStride;
+                ml[u] = make_float2(-INFINITY, 0.f);
+                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i < parts) {
+                  ml[u] = __ldcg(reinterpret_cast<const float2 *>(part + kMaxGroup * kHeadDim + 2 * h));
+                  v[u] = __ldcg(reinterpret_cast<const float4 *>(part + h * kHeadDim + col));
+                }
+              }
+              float top = M;
+#pragma unroll
+              for (int u = 0; u < kPaJoin; ++u) top = fmaxf(top, ml[u].x);
+              const float back = M == top ? 1.f : fast_exp2(M - top);
+              l *= back; o.x *= back; o.y *= back; o.z *= back; o.w *= back;
+              M = top;
+#pragma unroll
+              for (int u = 0; u < kPaJoin; ++u) {
+                const float f = ml[u].x == M ? 1.f : fast_exp2(ml[u].x - M);
+                l += ml[u].y * f;
+                o.x += v[u].x * f; o.y += v[u].y * f; o.z += v[u].z * f; o.w += v[u].w * f;
+              }
             }
-            finish(h, col, o, sh.ml[0][h].x, sh.ml[0][h].y);
+            finish(h, col, o, M, l);
           }
         }
       }
-      // ---- the next pair with tokens ----
-      pair_x0 += pair_tiles;
-      if (++at.head == p.H_kv) {
-        at.head = 0;
-        do at.len = tokens_of(p.c, ++at.seq);
-        while (at.len == 0 && at.seq < p.c.n_seqs);
-      }
+      SAGEKV_STAMP(8);
+      at.next_pair(p.c, p.H_kv, lens, lane);
     }
     if (timed_out) atomicOr(p.c.status, kStatusWaitTimeout);
   }
-
-  // ---- sequences without tokens ----
-  for (int s = blockIdx.x; s < p.c.n_seqs; s += n_ctas) {
-    if (tokens_of(p.c, s) > 0) continue;
-    for (int i = tid; i < p.H_q * (kHeadDim / 8); i += kPaThreads) st_v4(p.out + (int64_t)s * p.H_q * kHeadDim + i * 8, make_uint4(0u, 0u, 0u, 0u));
-    if (p.lse != nullptr)
-      for (int i = tid; i < p.H_q; i += kPaThreads) p.lse[(int64_t)s * p.H_q + i] = -INFINITY;
-  }
-}
-
-// [n_pages, H_kv, page_size, 128] through the cache's strides, boxes of 16 rows x 128 bytes with the 128-byte swizzle
-static bool make_page_map(CUtensorMap *map, uint8_t *base, const PagedAttnParams &p, bool e4m3) {
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (enc == nullptr) return false;
-  const cuuint64_t size = e4m3 ? 1 : 2;
-  const cuuint64_t dims[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)p.c.page_size, (cuuint64_t)p.H_kv, (cuuint64_t)p.c.n_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)p.c.token_stride * size, (cuuint64_t)p.c.head_stride * size, (cuuint64_t)p.c.page_stride * size};
-  const cuuint32_t box[4] = {e4m3 ? 128u : 64u, 16, 1, 1};
-  const cuuint32_t estr[4] = {1, 1, 1, 1};
-  return enc(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  SAGEKV_STAMP(9);
+  SAGEKV_TRACE_END(p.q);
 }
 
 cudaError_t paged_attn_setup() {
@@ -489,16 +471,15 @@ cudaError_t launch_paged_attn(const PagedAttnParams &p, int dtype, int n_sm, cud
   if (p.c.n_seqs <= 0) return cudaSuccess;
   const bool e4m3 = dtype == SAGEKV_CACHE_E4M3;
   CUtensorMap map_k, map_v;
-  if (!make_page_map(&map_k, p.c.k, p, e4m3) || !make_page_map(&map_v, p.c.v, p, e4m3)) return cudaErrorInvalidValue;
-  const int64_t most = (int64_t)p.c.n_seqs * p.H_kv * p.c.max_pages * (p.c.page_size / 16);   // tiles, if every sequence filled its table
-  int64_t ctas = (most + kPaMinTiles - 1) / kPaMinTiles;
-  int most_ctas = paged_attn_max_ctas(n_sm);
-  static_assert(kPaMaxParts >= 2 * 160, "a pair may be shared by every CTA");
-  if (most_ctas > kPaMaxParts) most_ctas = kPaMaxParts;
-  if (ctas > most_ctas) ctas = most_ctas;
+  if (!make_page_map(&map_k, p.c.k, p.c, p.H_kv, e4m3) || !make_page_map(&map_v, p.c.v, p.c, p.H_kv, e4m3)) return cudaErrorInvalidValue;
+  const int64_t most_units = ((int64_t)p.c.max_pages * p.c.page_size + 16 * kPaWarps - 1) / (16 * kPaWarps);   // of a sequence that fills its table
+  int64_t ctas = (p.c.n_seqs * p.H_kv * (most_units + kPaPairCost) + kPaMinPlaces - 1) / kPaMinPlaces;
+  if (ctas > paged_attn_max_ctas(n_sm)) ctas = paged_attn_max_ctas(n_sm);
   if (ctas < 1) ctas = 1;
   return launch_next(e4m3 ? paged_attn_kernel<true> : paged_attn_kernel<false>, dim3((unsigned)ctas), kPaThreads, sizeof(PaShared), stream, 0,
                      p, map_k, map_v);
 }
 
 }  // namespace sagekv
+
+SAGEKV_TRACE_READER(sagekv_trace_read_paged)

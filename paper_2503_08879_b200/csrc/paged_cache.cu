@@ -1,7 +1,6 @@
 // What fills a paged cache and what reduces it:
 //   rope      rows of queries or keys rotated by their positions;
 //   append    keys and values of new tokens into their pages, the keys rotated on the way, the tokens' queries beside;
-//   score     Step 2 of the method (first half) on pages: sagekv_score with a table between a token and its row;
 //   compact   Step 3 on pages: the reduced cache from the kept positions.
 // All are bound by memory: every row is read once and written once, 16 bytes per access.
 #include "paged.cuh"
@@ -159,65 +158,67 @@ __global__ void __launch_bounds__(kRopeWarps * 32) paged_append_kernel(const __g
   const int quad0 = (int)(job - t * warps_per_token) * quads;
   const int pa = first_piece(p.rope, piece) * 8, pb = second_piece(p.rope, piece) * 8;
   const int position = p.positions[t];
-  if (position < 0) return;                                    // a place without a token
-  // the token's page: where any of position, sequence and page id is out of range its rows have no place
   const int64_t seq = p.seqs != nullptr ? (int64_t)p.seqs[t] : t;
-  int64_t row = -1;
-  if (seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size) {
-    const int entry = page_of(position, p.c.page_size, p.c.page_magic);
-    row = paged_row(p.c.table[seq * p.c.table_stride + entry], p.c.n_pages, position - entry * p.c.page_size, 0, p.c.page_stride, 0,
-                    p.c.token_stride);
-  }
-  if (row < 0 && lane == 0) atomicOr(p.c.status, kStatusBounds);
-  Angles a;
-  bool have = false;
-  for (int q0 = quad0; q0 < min(quad0 + quads, all_quads); q0 += kRopeQuads) {
-    uint4 xa[kRopeQuads], xb[kRopeQuads];
-    int head[kRopeQuads], kind[kRopeQuads];                    // kind 0: a query, 1: a key, 2: a value; head -1: nothing
+  uint4 xa[kRopeQuads], xb[kRopeQuads];
+  int head[kRopeQuads], kind[kRopeQuads];                      // kind 0: a query, 1: a key, 2: a value; head -1: nothing
+  float scale[kRopeQuads];
+  auto load = [&](int q0) {
 #pragma unroll
     for (int u = 0; u < kRopeQuads; ++u) {
       const int quad = q0 + u;
       kind[u] = quad < q_quads ? 0 : quad < q_quads + kv_quads ? 1 : 2;
       head[u] = (quad - (kind[u] == 0 ? 0 : q_quads + (kind[u] - 1) * kv_quads)) * 4 + group;
       if (quad >= min(quad0 + quads, all_quads) || head[u] >= (kind[u] == 0 ? p.H_q : p.H_kv)) head[u] = -1;
+      scale[u] = 1.f;
       if (head[u] >= 0) {
         const uint16_t *x = kind[u] == 0 ? p.q + t * p.q_token + (int64_t)head[u] * p.q_head
                                          : (kind[u] == 1 ? p.k : p.v) + t * p.kv_token + (int64_t)head[u] * p.kv_head;
         xa[u] = ld_v4(x + pa);
         xb[u] = ld_v4(x + pb);
+        if (kE4m3 && kind[u] != 0) {
+          const float *scales = kind[u] == 1 ? p.c.k_scale : p.c.v_scale;
+          if (scales != nullptr) scale[u] = scales[head[u]];
+        }
       }
     }
-    if (!have && p.rope.rotary_dim > 0 && q0 < q_quads + kv_quads) { angles_of(p.rope, position, lane, a); have = true; }
+  };
+  load(quad0);                                                 // on their way while the page is looked up
+  if (position < 0) return;                                    // a place without a token
+  // the token's page: where any of position, sequence and page id is out of range its rows have no place
+  int page = -1, slot = 0;
+  bool in_table = seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size;
+  if (in_table) {
+    const int entry = page_of(position, p.c.page_size, p.c.page_magic);
+    slot = position - entry * p.c.page_size;
+    page = p.c.table[seq * p.c.table_stride + entry];
+  }
+  Angles a;
+  if (p.rope.rotary_dim > 0 && quad0 < q_quads + kv_quads) angles_of(p.rope, position, lane, a);
+  const int64_t row = paged_row(page, p.c.n_pages, slot, 0, p.c.page_stride, 0, p.c.token_stride);
+  if (row < 0 && lane == 0) atomicOr(p.c.status, kStatusBounds);
+  for (int q0 = quad0; q0 < min(quad0 + quads, all_quads); q0 += kRopeQuads) {
+    if (q0 > quad0) load(q0);
 #pragma unroll
     for (int u = 0; u < kRopeQuads; ++u) {
       if (head[u] < 0 || (kind[u] != 0 && row < 0)) continue;
       float y[16];
       const bool as_is = kind[u] == 2 || p.rope.rotary_dim == 0;
-      if (as_is && kind[u] == 0) {
+      if (!as_is) rotate(p.rope, a, piece, xa[u], xb[u], y);
+      if (kind[u] == 0) {
         uint16_t *o = p.q_out + t * p.q_out_token + (int64_t)head[u] * p.q_out_head;
-        st_v4(o + pa, xa[u]);
-        st_v4(o + pb, xb[u]);
+        st_v4(o + pa, as_is ? xa[u] : pack8_bf16(y));
+        st_v4(o + pb, as_is ? xb[u] : pack8_bf16(y + 8));
         continue;
-      }
-      if (!as_is) {
-        rotate(p.rope, a, piece, xa[u], xb[u], y);
-        if (kind[u] == 0) {
-          uint16_t *o = p.q_out + t * p.q_out_token + (int64_t)head[u] * p.q_out_head;
-          st_v4(o + pa, pack8_bf16(y));
-          st_v4(o + pb, pack8_bf16(y + 8));
-          continue;
-        }
       }
       uint8_t *pages = kind[u] == 1 ? p.c.k : p.c.v;
       const int64_t at = row + (int64_t)head[u] * p.c.head_stride;
       if (kE4m3) {
-        const float *scale = kind[u] == 1 ? p.c.k_scale : p.c.v_scale;
-        const float inv = scale != nullptr ? 1.f / scale[head[u]] : 1.f;
         if (as_is) {
           const uint32_t w[8] = {xa[u].x, xa[u].y, xa[u].z, xa[u].w, xb[u].x, xb[u].y, xb[u].z, xb[u].w};
 #pragma unroll
           for (int i = 0; i < 8; ++i) { y[2 * i] = bf16_low(w[i]); y[2 * i + 1] = bf16_high(w[i]); }
         }
+        const float inv = 1.f / scale[u];
         *reinterpret_cast<uint2 *>(pages + at + pa) = pack8_e4m3(y, inv);
         *reinterpret_cast<uint2 *>(pages + at + pb) = pack8_e4m3(y + 8, inv);
       } else {
@@ -239,240 +240,88 @@ cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm,
                      kRopeWarps * 32, 0, stream, 0, p, quads, warps);
 }
 
-// ---- score -----------------------------------------------------------------------------------------------------------
-// The first pass of the score step (see score.cu: a warp's tiles go from global memory straight into matrix fragments,
-// all loads in flight), with every lane looking up the pages of its own two rows per tile.  An 8-bit row is half as
-// long, so a warp takes twice as many tiles: the bytes in flight are what the memory's latency needs.  Writes the scaled logits and
-// a (max, sum) pair per CTA and head; the second pass is the score step's own.
-template <bool kE4m3>
-__global__ void __launch_bounds__(kScoreWarps * 32, 2) paged_score_kernel(const ScoreParams p, const PagedView c) {
-  constexpr int kTiles = kE4m3 ? 2 * kScoreTiles : kScoreTiles;
-  constexpr int kPieces = kE4m3 ? 2 : 4;                       // 16-byte pieces of a row that a lane holds
-  const int chunk = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = lane >> 2, cc = lane & 3;
-  wait_for_predecessor();
-  if (chunk == 0 && p.sketch_off >= 0) {                       // the rows' histograms are filled by atomic adds in the second pass
-    for (int i = threadIdx.x; i < p.G * (kSketchBins + 4); i += kScoreWarps * 32) {
-      const int h = i / (kSketchBins + 4);
-      reinterpret_cast<uint32_t *>(p.scores + ((int64_t)b * p.H_q + kvh * p.G + h) * p.row_stride + p.sketch_off)[i - h * (kSketchBins + 4)] = 0u;
-    }
-  }
-
-  const int tok_base = (chunk * kScoreWarps + warp) * 16 * kTiles;
-  const int last = p.E - 1;
-  const int32_t *table = c.table + (int64_t)b * c.table_stride;
-  const uint8_t *head = c.k + (int64_t)kvh * c.head_stride * (kE4m3 ? 1 : 2);
-  int ids[kTiles][2];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) ids[t][e] = table[page_of(p.S + min(tok_base + t * 16 + g + 8 * e, last), c.page_size, c.page_magic)];
-  uint4 k[kTiles][2][kPieces];
-  uint32_t absent = 0u;                                        // bit 2t + e: no such page
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int tok = p.S + min(tok_base + t * 16 + g + 8 * e, last);
-      const int64_t row = paged_row(ids[t][e], c.n_pages, tok - page_of(tok, c.page_size, c.page_magic) * c.page_size, 0, c.page_stride, 0, c.token_stride);
-      if (row < 0) absent |= 1u << (2 * t + e);
-      const uint8_t *src = head + row * (kE4m3 ? 1 : 2) + cc * 16;
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) k[t][e][j] = row >= 0 ? ld_stream_v4(src + j * 64) : make_uint4(0u, 0u, 0u, 0u);
-    }
-  if (absent != 0u) atomicOr(c.status, kStatusBounds);
-
-  // B fragments: query head (kvh*G + g) for n = g, zero padding for n >= G; the dims as the pieces hold them
-  uint32_t qf[8][2];
-  const int h0 = 2 * cc, h1 = 2 * cc + 1;
-  float mult0 = p.scale_log2, mult1 = p.scale_log2;
-  {
-    const uint16_t *qrow = p.q + ((int64_t)b * p.H_q + kvh * p.G + min(g, p.G - 1)) * kHeadDim;
-    float largest = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      // bf16: piece j of a row holds dims 32j + 8cc .. + 7; 8-bit: piece j / 2 holds 64(j / 2) + 16cc .. + 15, eight of them here
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (g < p.G) v = ld_v4(qrow + (kE4m3 ? (j >> 1) * 64 + cc * 16 + (j & 1) * 8 : j * 32 + cc * 8));
-      qf[2 * j][0] = v.x; qf[2 * j][1] = v.y; qf[2 * j + 1][0] = v.z; qf[2 * j + 1][1] = v.w;
-    }
-    if (kE4m3) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) largest = fmaxf(largest, fmaxf(fabsf(bf16_low(qf[j][e])), fabsf(bf16_high(qf[j][e]))));
-      largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
-      largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
-      const int ex = query_exponent(largest);
-      const float up = power_of_two(ex);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) qf[j][e] = pack_f16x2(bf16_low(qf[j][e]) * up, bf16_high(qf[j][e]) * up);
-      const float base = c.k_scale != nullptr ? p.scale_log2 * c.k_scale[kvh] : p.scale_log2;
-      mult0 = base * power_of_two(-__shfl_sync(0xffffffffu, ex, h0 * 4));
-      mult1 = base * power_of_two(-__shfl_sync(0xffffffffu, ex, h1 * 4));
-    }
-  }
-
-  // running softmax statistics of heads 2cc and 2cc+1 over the rows this lane sees
-  float m0 = -INFINITY, l0 = 0.f, m1 = -INFINITY, l1 = 0.f;
-  float *row0 = p.scores + ((int64_t)b * p.H_q + kvh * p.G + h0) * p.row_stride;
-  float *row1 = row0 + p.row_stride;
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const uint32_t wa[4] = {k[t][0][j].x, k[t][0][j].y, k[t][0][j].z, k[t][0][j].w};
-      const uint32_t wb[4] = {k[t][1][j].x, k[t][1][j].y, k[t][1][j].z, k[t][1][j].w};
-      if (kE4m3) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          mma_f16_16816(a0, a1, a2, a3, f16x2_low(wa[w]), f16x2_low(wb[w]), f16x2_high(wa[w]), f16x2_high(wb[w]), qf[4 * j + w][0], qf[4 * j + w][1]);
-      } else {
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-          mma_bf16_16816(a0, a1, a2, a3, wa[2 * w], wb[2 * w], wa[2 * w + 1], wb[2 * w + 1], qf[2 * j + w][0], qf[2 * j + w][1]);
-      }
-    }
-    const int r0 = tok_base + t * 16 + g, r1 = r0 + 8;
-    const bool ok0 = !((absent >> (2 * t)) & 1u), ok1 = !((absent >> (2 * t + 1)) & 1u);   // a row that is not there gets no weight
-    const float s00 = ok0 ? a0 * mult0 : -INFINITY, s01 = ok0 ? a1 * mult1 : -INFINITY;   // (r0,h0) (r0,h1)
-    const float s10 = ok1 ? a2 * mult0 : -INFINITY, s11 = ok1 ? a3 * mult1 : -INFINITY;   // (r1,h0) (r1,h1)
-    const bool v0 = r0 < p.E && SAGEKV_OK_INDEX(p.status, r0 >= 0 && (int64_t)r0 < p.row_stride);
-    const bool v1 = r1 < p.E && SAGEKV_OK_INDEX(p.status, r1 >= 0 && (int64_t)r1 < p.row_stride);
-    if (h0 < p.G) {
-      if (v0) row0[r0] = s00;
-      if (v1) row0[r1] = s10;
-      const float x0 = v0 ? s00 : -INFINITY, x1 = v1 ? s10 : -INFINITY;
-      const float M = fmaxf(m0, fmaxf(x0, x1));
-      if (M != -INFINITY) l0 = l0 * fast_exp2(m0 - M) + fast_exp2(x0 - M) + fast_exp2(x1 - M);
-      m0 = M;
-    }
-    if (h1 < p.G) {
-      if (v0) row1[r0] = s01;
-      if (v1) row1[r1] = s11;
-      const float x0 = v0 ? s01 : -INFINITY, x1 = v1 ? s11 : -INFINITY;
-      const float M = fmaxf(m1, fmaxf(x0, x1));
-      if (M != -INFINITY) l1 = l1 * fast_exp2(m1 - M) + fast_exp2(x0 - M) + fast_exp2(x1 - M);
-      m1 = M;
-    }
-  }
-  // over the 8 row groups of the warp (lanes with equal cc), then over the warps
-#pragma unroll
-  for (int off = 4; off < 32; off <<= 1) {
-    merge_ml(m0, l0, __shfl_xor_sync(0xffffffffu, m0, off), __shfl_xor_sync(0xffffffffu, l0, off));
-    merge_ml(m1, l1, __shfl_xor_sync(0xffffffffu, m1, off), __shfl_xor_sync(0xffffffffu, l1, off));
-  }
-  __shared__ float2 sm[kScoreWarps][kMaxGroup];
-  if (g == 0) {
-    sm[warp][h0] = make_float2(m0, l0);
-    sm[warp][h1] = make_float2(m1, l1);
-  }
-  __syncthreads();
-  if (threadIdx.x < p.G) {
-    const int h = threadIdx.x;
-    float m = sm[0][h].x, l = sm[0][h].y;
-#pragma unroll
-    for (int w = 1; w < kScoreWarps; ++w) merge_ml(m, l, sm[w][h].x, sm[w][h].y);
-    if (SAGEKV_OK_INDEX(p.status, chunk < p.n_chunks && kvh * p.G + h < p.H_q))
-      p.partials[((int64_t)b * p.H_q + kvh * p.G + h) * p.n_chunks + chunk] = make_float2(m, l);
-  }
-}
-
-cudaError_t launch_paged_score(ScoreParams p, const PagedView &c, int dtype, int n_sm, cudaStream_t stream) {
-  if (p.E <= 0) return cudaSuccess;
-  const bool e4m3 = dtype == SAGEKV_CACHE_E4M3;
-  const int per_cta = kScoreChunk * (e4m3 ? 2 : 1);
-  p.n_chunks = (p.E + per_cta - 1) / per_cta;
-  p.sketch_off = score_sketch_offset(p);
-  const cudaError_t e = launch_next(e4m3 ? paged_score_kernel<true> : paged_score_kernel<false>,
-                                    dim3((unsigned)p.n_chunks, (unsigned)p.H_kv, (unsigned)p.B), kScoreWarps * 32, 0, stream, 0, p, c);
-  return e != cudaSuccess ? e : launch_score_normalise(p, n_sm, stream);
-}
-
 // ---- compact ---------------------------------------------------------------------------------------------------------
-// Rows as in sagekv_select_compact: sink, the G lists, recent tokens, last token.  A warp takes kCompactRows rows, K by its
-// lower half and V by its upper one; their chain of three loads (list, table, row) runs for all of them together.  An
-// 8-bit row is widened: code * scale, rounded to bf16.
+// Rows as in sagekv_select_compact: sink, the G lists, recent tokens, last token.  A warp takes up to 32 rows of one KV head:
+// each lane finds one row's place (list, then table: two loads one behind the other, for all rows at once), then the
+// rows are moved kCompactRows at a time, 16 bytes per lane, all loads ahead of the stores.  An 8-bit row is widened: code * scale,
+// rounded to bf16.
 constexpr int kCompactWarps = 8;
-constexpr int kCompactRows = 4;
+constexpr int kCompactRows = 8;
 
 template <bool kE4m3>
-__global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const PagedCompactParams p) {
-  const int lane = threadIdx.x & 31, piece = lane & 15;
-  const bool is_v = lane >= 16;
+__global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const PagedCompactParams p, const int rows_per_warp) {
+  constexpr int kLanes = kE4m3 ? 8 : 16;                       // of a row of K or of V
+  constexpr int kAtOnce = 32 / (2 * kLanes);                   // rows of K and V that a load instruction covers
+  constexpr int kLoads = kCompactRows / kAtOnce;
+  const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1);
+  const bool is_v = (lane / kLanes) & 1;
+  const int sub = lane / (2 * kLanes);                         // which of the rows of a load
   wait_for_predecessor();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.d_step = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.d_step = 0;
   const int n_sel = p.G * p.k_q, L = p.S + n_sel + p.R + 1;
-  const int64_t n_rows = (int64_t)p.B * p.H_kv * L;
+  const int bk = blockIdx.y, b = bk / p.H_kv, kvh = bk - b * p.H_kv;
+  const int first = (int)(blockIdx.x * kCompactWarps + (threadIdx.x >> 5)) * rows_per_warp, n = min(rows_per_warp, L - first);
+  if (n <= 0) return;
+  int64_t src = -1;                                            // lane i: the place of row first + i, -1: there is none
+  if (lane < n) {
+    const int r = first + lane;
+    int tok = r < p.S ? r : p.N - L + r;
+    if (r >= p.S && r < p.S + n_sel) {                         // the lists of a KV head's query heads lie one behind the other, as its segments do
+      const int off = p.idx[(int64_t)bk * n_sel + (r - p.S)];
+      tok = off >= 0 && off < p.E ? p.S + off : -1;
+    }
+    if (tok >= 0) {
+      const int entry = page_of(tok, p.c.page_size, p.c.page_magic);
+      src = paged_row(p.c.table[(int64_t)b * p.c.table_stride + entry], p.c.n_pages, tok - entry * p.c.page_size, kvh, p.c.page_stride,
+                      p.c.head_stride, p.c.token_stride);
+    }
+    if (src < 0) atomicOr(p.c.status, kStatusBounds);          // a position or a page id out of range: the row is left as it was
+  }
   const uint8_t *pages = is_v ? p.c.v : p.c.k;
-  uint16_t *dst = is_v ? p.Vc : p.Kc;
   const float *scales = is_v ? p.c.v_scale : p.c.k_scale;
-  const int64_t first = ((int64_t)blockIdx.x * kCompactWarps + (threadIdx.x >> 5)) * kCompactRows;
-  int tok[kCompactRows], b[kCompactRows], kvh[kCompactRows], r[kCompactRows], page[kCompactRows];
+  const float scale = kE4m3 && scales != nullptr ? scales[kvh] : 1.f;
+  uint16_t *dst = (is_v ? p.Vc : p.Kc) + (int64_t)b * p.cs.batch_stride + (int64_t)kvh * p.cs.head_stride + (int64_t)first * p.cs.token_stride +
+                  piece * (128 / kLanes);
+  for (int i0 = 0; i0 < n; i0 += kCompactRows) {
+    uint4 row[kLoads];
+    bool there[kLoads];
 #pragma unroll
-  for (int u = 0; u < kCompactRows; ++u) {
-    tok[u] = -1;
-    if (first + u >= n_rows) continue;
-    const int bk = (int)((first + u) / L);
-    r[u] = (int)(first + u - (int64_t)bk * L);
-    b[u] = bk / p.H_kv;
-    kvh[u] = bk - b[u] * p.H_kv;
-    if (r[u] < p.S) tok[u] = r[u];
-    else if (r[u] >= p.S + n_sel) tok[u] = p.N - L + r[u];
-    else {
-      // the lists of a KV head's query heads lie one behind the other, as its segments do
-      const int off = p.idx[(int64_t)bk * n_sel + (r[u] - p.S)];
-      tok[u] = off >= 0 && off < p.E ? p.S + off : -2;
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = i0 + u * kAtOnce + sub;
+      const int64_t at = __shfl_sync(0xffffffffu, src, i & 31);
+      there[u] = i < n && at >= 0;
+      if (there[u]) row[u] = ld_stream_v4(pages + at * (kE4m3 ? 1 : 2) + piece * 16);
     }
-  }
 #pragma unroll
-  for (int u = 0; u < kCompactRows; ++u)
-    page[u] = tok[u] >= 0 ? p.c.table[(int64_t)b[u] * p.c.table_stride + page_of(tok[u], p.c.page_size, p.c.page_magic)] : -1;
-  uint4 row[kCompactRows];
+    for (int u = 0; u < kLoads; ++u) {
+      if (!there[u]) continue;
+      uint16_t *o = dst + (int64_t)(i0 + u * kAtOnce + sub) * p.cs.token_stride;
+      if (kE4m3) {
+        const uint32_t w[4] = {row[u].x, row[u].y, row[u].z, row[u].w};
+        uint32_t y[8];
 #pragma unroll
-  for (int u = 0; u < kCompactRows; ++u) {
-    if (tok[u] == -1) continue;
-    const int64_t src = tok[u] < 0 ? -1 : paged_row(page[u], p.c.n_pages, tok[u] - page_of(tok[u], p.c.page_size, p.c.page_magic) * p.c.page_size,
-                                                   kvh[u], p.c.page_stride, p.c.head_stride, p.c.token_stride);
-    if (src < 0) {                                             // a position or a page id out of range: the row is left as it was
-      tok[u] = -1;
-      if (lane == 0) atomicOr(p.c.status, kStatusBounds);
-    } else if (kE4m3) {
-      const uint2 v = *reinterpret_cast<const uint2 *>(pages + src + piece * 8);
-      row[u].x = v.x; row[u].y = v.y;
-    } else {
-      row[u] = ld_stream_v4(reinterpret_cast<const uint16_t *>(pages) + src + piece * 8);
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < kCompactRows; ++u) {
-    if (tok[u] == -1) continue;
-    if (kE4m3) {
-      const float scale = scales != nullptr ? scales[kvh[u]] : 1.f;
-      const uint32_t w[4] = {f16x2_low(row[u].x), f16x2_high(row[u].x), f16x2_low(row[u].y), f16x2_high(row[u].y)};
-      uint32_t y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 x = float2_of_f16x2(w[i]);
-        y[i] = pack_bf16x2(x.x * scale, x.y * scale);
+        for (int i = 0; i < 4; ++i) {
+          const float2 x0 = float2_of_f16x2(f16x2_low(w[i])), x1 = float2_of_f16x2(f16x2_high(w[i]));
+          y[2 * i] = pack_bf16x2(x0.x * scale, x0.y * scale);
+          y[2 * i + 1] = pack_bf16x2(x1.x * scale, x1.y * scale);
+        }
+        st_v4(o, make_uint4(y[0], y[1], y[2], y[3]));
+        st_v4(o + 8, make_uint4(y[4], y[5], y[6], y[7]));
+      } else {
+        st_v4(o, row[u]);
       }
-      row[u] = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    st_v4(dst + (int64_t)b[u] * p.cs.batch_stride + (int64_t)kvh[u] * p.cs.head_stride + (int64_t)r[u] * p.cs.token_stride + piece * 8, row[u]);
   }
 }
 
 cudaError_t launch_paged_compact(const PagedCompactParams &p, int dtype, int n_sm, cudaStream_t stream) {
-  (void)n_sm;
-  const int64_t n_rows = (int64_t)p.B * p.H_kv * (p.S + (int64_t)p.G * p.k_q + p.R + 1);
-  const int64_t per_block = kCompactWarps * kCompactRows, blocks = (n_rows + per_block - 1) / per_block;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_next(dtype == SAGEKV_CACHE_E4M3 ? paged_compact_kernel<true> : paged_compact_kernel<false>, dim3((unsigned)blocks),
-                     kCompactWarps * 32, 0, stream, 0, p);
+  const int64_t L = p.S + (int64_t)p.G * p.k_q + p.R + 1, heads = (int64_t)p.B * p.H_kv;
+  // as many rows per warp as leave every SM a dozen warps
+  int rows = kCompactRows;
+  while (rows < 32 && L * heads / (2 * rows) >= (int64_t)n_sm * 12) rows *= 2;
+  const int64_t per_block = (int64_t)kCompactWarps * rows;
+  return launch_next(dtype == SAGEKV_CACHE_E4M3 ? paged_compact_kernel<true> : paged_compact_kernel<false>,
+                     dim3((unsigned)((L + per_block - 1) / per_block), (unsigned)heads), kCompactWarps * 32, 0, stream, 0, p, rows);
 }
 
 }  // namespace sagekv
