@@ -60,17 +60,6 @@ struct RopeArgs {
   int rotary_dim, interleaved;
   float amplitude;
 };
-struct RopeParams {
-  RopeArgs rope;
-  const uint16_t *x;
-  uint16_t *out;
-  int64_t x_token, x_head, out_token, out_head;
-  const int32_t *positions;
-  int64_t n_tokens;
-  int n_heads;
-};
-cudaError_t launch_rope(const RopeParams &p, int n_sm, cudaStream_t stream);
-
 struct PagedAppendParams {
   RopeArgs rope;                  // rotary_dim 0: nothing turns
   PagedView c;
@@ -81,6 +70,7 @@ struct PagedAppendParams {
   int64_t n_tokens;
   int H_q, H_kv;
 };
+cudaError_t launch_rope(const PagedAppendParams &p, int n_sm, cudaStream_t stream);   // the queries alone (H_q of them; every position counts)
 cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm, cudaStream_t stream);
 
 // p.K and p.ks are unused; p.n_chunks (at most max_chunks) is set here

@@ -154,17 +154,17 @@ int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sa
   if (x == nullptr || out == nullptr || positions == nullptr || !rows_apart(xs, n_tokens, n_heads) || !rows_apart(os, n_tokens, n_heads))
     return SAGEKV_ERR_INVALID;
   if (!aligned16(x) || !aligned16(out) || !rows_aligned(xs) || !rows_aligned(os)) return SAGEKV_ERR_ALIGN;
-  RopeParams p;
+  PagedAppendParams p = {};
   p.rope = rope_args(plan);
-  p.x = static_cast<const uint16_t *>(x);
-  p.out = static_cast<uint16_t *>(out);
-  p.x_token = xs.token_stride;
-  p.x_head = xs.head_stride;
-  p.out_token = os.token_stride;
-  p.out_head = os.head_stride;
+  p.q = static_cast<const uint16_t *>(x);
+  p.q_out = static_cast<uint16_t *>(out);
+  p.q_token = xs.token_stride;
+  p.q_head = xs.head_stride;
+  p.q_out_token = os.token_stride;
+  p.q_out_head = os.head_stride;
   p.positions = positions;
   p.n_tokens = n_tokens;
-  p.n_heads = n_heads;
+  p.H_q = n_heads;
   return done(ctx, launch_rope(p, ctx->dev->n_sm, static_cast<cudaStream_t>(stream)));
 }
 

@@ -30,229 +30,246 @@ __device__ __forceinline__ int second_piece(const RopeArgs &r, int p) {
   return p + turning;
 }
 
+// two 32-bit numbers side by side, as the packed instructions take them
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(f32x2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 struct Angles {
-  float cs[8], sn[8];
+  f32x2 cs[4], sn[4], ns[4];   // cosines, sines and negated sines of a lane's eight pairs
 };
 
 // lane: p = lane & 7, group = lane >> 3; all lanes take part
-__device__ __forceinline__ void angles_of(const RopeArgs &r, int position, int lane, Angles &a) {
+__device__ __forceinline__ void angles_of(const uint64_t *turns, float amplitude, int position, int lane, Angles &a) {
   const int p = lane & 7, group = lane >> 3;
   float cs[2], sn[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const uint64_t revolutions = r.turns[8 * p + 2 * group + e] * (uint64_t)(int64_t)position;
+    const uint64_t revolutions = turns[8 * p + 2 * group + e] * (uint64_t)(int64_t)position;
     const int half = (int)(uint32_t)((revolutions + 0x80000000ull) >> 32);      // in 2^-31 half revolutions, signed
     sincospif((float)half * 0x1p-31f, &sn[e], &cs[e]);
-    cs[e] *= r.amplitude;
-    sn[e] *= r.amplitude;
+    cs[e] *= amplitude;
+    sn[e] *= amplitude;
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    a.cs[e] = __shfl_sync(0xffffffffu, cs[e & 1], (e >> 1) * 8 + p);
-    a.sn[e] = __shfl_sync(0xffffffffu, sn[e & 1], (e >> 1) * 8 + p);
+  for (int e = 0; e < 4; ++e) {
+    float c[2], s[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c[i] = __shfl_sync(0xffffffffu, cs[i], e * 8 + p);
+      s[i] = __shfl_sync(0xffffffffu, sn[i], e * 8 + p);
+    }
+    a.cs[e] = pack2(c[0], c[1]);
+    a.sn[e] = pack2(s[0], s[1]);
+    a.ns[e] = pack2(-s[0], -s[1]);
   }
 }
 
-// the sixteen values of a lane's two pieces, rotated where the lane's pairs turn
-__device__ __forceinline__ void rotate(const RopeArgs &r, const Angles &a, int p, uint4 first, uint4 second, float (&y)[16]) {
+__device__ __forceinline__ f32x2 widen(uint32_t w) { return pack2(bf16_low(w), bf16_high(w)); }
+
+// the sixteen values of a lane's two pieces (eight twos), rotated
+__device__ __forceinline__ void rotate(const RopeArgs &r, const Angles &a, const uint4 &first, const uint4 &second, f32x2 (&y)[8]) {
   const uint32_t w[8] = {first.x, first.y, first.z, first.w, second.x, second.y, second.z, second.w};
-  float x[16];
+  if (r.interleaved) {                                         // a word holds a pair
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { x[2 * i] = bf16_low(w[i]); x[2 * i + 1] = bf16_high(w[i]); }
-  if (p < (r.rotary_dim >> 4)) {
-    if (r.interleaved) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[2 * e] = x[2 * e] * a.cs[e] - x[2 * e + 1] * a.sn[e];
-        y[2 * e + 1] = x[2 * e + 1] * a.cs[e] + x[2 * e] * a.sn[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = x[e] * a.cs[e] - x[8 + e] * a.sn[e];
-        y[8 + e] = x[8 + e] * a.cs[e] + x[e] * a.sn[e];
-      }
+    for (int e = 0; e < 8; ++e) {
+      const float2 c2 = unpack2(a.cs[e >> 1]), s2 = unpack2(a.sn[e >> 1]);
+      const float c = e & 1 ? c2.y : c2.x, s = e & 1 ? s2.y : s2.x, lo = bf16_low(w[e]), hi = bf16_high(w[e]);
+      y[e] = pack2(lo * c - hi * s, hi * c + lo * s);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = x[i];
+    for (int e = 0; e < 4; ++e) {
+      const f32x2 lo = widen(w[e]), hi = widen(w[4 + e]);
+      y[e] = fma2(hi, a.ns[e], mul2(lo, a.cs[e]));
+      y[4 + e] = fma2(lo, a.sn[e], mul2(hi, a.cs[e]));
+    }
   }
 }
 
-__device__ __forceinline__ uint4 pack8_bf16(const float *y) {
-  return make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-}
-__device__ __forceinline__ uint2 pack8_e4m3(const float *y, float inv_scale) {
+__device__ __forceinline__ uint4 pack8_bf16(const f32x2 *y) {
   uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = pack_e4m3x2(y[2 * i] * inv_scale, y[2 * i + 1] * inv_scale);
-  return make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
-}
-
-constexpr int kRopeWarps = 8;
-constexpr int kRopeQuads = 4;   // groups of four rows a warp loads before it stores any
-
-// A warp takes `quads` groups of four heads of one token.
-__global__ void __launch_bounds__(kRopeWarps * 32) rope_kernel(const __grid_constant__ RopeParams p, const int quads, const int warps_per_token) {
-  const int lane = threadIdx.x & 31, piece = lane & 7, group = lane >> 3;
-  const int64_t job = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
-  wait_for_predecessor();
-  const int64_t t = job / warps_per_token;
-  if (t >= p.n_tokens) return;
-  const int quad0 = (int)(job - t * warps_per_token) * quads, all_quads = (p.n_heads + 3) >> 2;
-  const int pa = first_piece(p.rope, piece) * 8, pb = second_piece(p.rope, piece) * 8;
-  const uint16_t *x = p.x + t * p.x_token;
-  uint16_t *out = p.out + t * p.out_token;
-  const int position = p.positions[t];
-  Angles a;
-  bool have = false;
-  for (int q0 = quad0; q0 < min(quad0 + quads, all_quads); q0 += kRopeQuads) {
-    uint4 xa[kRopeQuads], xb[kRopeQuads];
-#pragma unroll
-    for (int u = 0; u < kRopeQuads; ++u) {
-      const int h = (q0 + u) * 4 + group;
-      if (q0 + u < quad0 + quads && h < p.n_heads) {
-        xa[u] = ld_v4(x + (int64_t)h * p.x_head + pa);
-        xb[u] = ld_v4(x + (int64_t)h * p.x_head + pb);
-      }
-    }
-    if (!have) { angles_of(p.rope, position, lane, a); have = true; }
-#pragma unroll
-    for (int u = 0; u < kRopeQuads; ++u) {
-      const int h = (q0 + u) * 4 + group;
-      if (q0 + u < quad0 + quads && h < p.n_heads) {
-        float y[16];
-        rotate(p.rope, a, piece, xa[u], xb[u], y);
-        st_v4(out + (int64_t)h * p.out_head + pa, pack8_bf16(y));
-        st_v4(out + (int64_t)h * p.out_head + pb, pack8_bf16(y + 8));
-      }
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = unpack2(y[i]);
+    w[i] = pack_bf16x2(v.x, v.y);
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-
-// groups of four rows per warp: one where there are few (latency), up to all of a token's where the device is full
-static int quads_per_warp(int64_t tokens, int quads, int n_sm) {
-  int64_t n = tokens * quads / ((int64_t)n_sm * 32);
-  return (int)(n < 1 ? 1 : n > quads ? quads : n);
-}
-
-cudaError_t launch_rope(const RopeParams &p, int n_sm, cudaStream_t stream) {
-  if (p.n_tokens <= 0 || p.n_heads <= 0) return cudaSuccess;
-  const int all = (p.n_heads + 3) / 4, quads = quads_per_warp(p.n_tokens, all, n_sm), warps = (all + quads - 1) / quads;
-  const int64_t blocks = (p.n_tokens * warps + kRopeWarps - 1) / kRopeWarps;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_next(rope_kernel, dim3((unsigned)blocks), kRopeWarps * 32, 0, stream, 0, p, quads, warps);
-}
-
-// ---- append ----------------------------------------------------------------------------------------------------------
-// As rope, over the groups of four rows of a token's queries, keys and values in this order.
-template <bool kE4m3>
-__global__ void __launch_bounds__(kRopeWarps * 32) paged_append_kernel(const __grid_constant__ PagedAppendParams p, const int quads,
-                                                                       const int warps_per_token) {
-  const int lane = threadIdx.x & 31, piece = lane & 7, group = lane >> 3;
-  const int64_t job = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
-  wait_for_predecessor();
-  const int64_t t = job / warps_per_token;
-  if (t >= p.n_tokens) return;
-  const int q_quads = p.q != nullptr ? (p.H_q + 3) >> 2 : 0, kv_quads = (p.H_kv + 3) >> 2, all_quads = q_quads + 2 * kv_quads;
-  const int quad0 = (int)(job - t * warps_per_token) * quads;
-  const int pa = first_piece(p.rope, piece) * 8, pb = second_piece(p.rope, piece) * 8;
-  const int position = p.positions[t];
-  const int64_t seq = p.seqs != nullptr ? (int64_t)p.seqs[t] : t;
-  uint4 xa[kRopeQuads], xb[kRopeQuads];
-  int head[kRopeQuads], kind[kRopeQuads];                      // kind 0: a query, 1: a key, 2: a value; head -1: nothing
-  float scale[kRopeQuads];
-  auto load = [&](int q0) {
+__device__ __forceinline__ uint2 pack8_e4m3(const f32x2 *y, f32x2 inv_scale) {
+  uint32_t w[4];
 #pragma unroll
-    for (int u = 0; u < kRopeQuads; ++u) {
-      const int quad = q0 + u;
-      kind[u] = quad < q_quads ? 0 : quad < q_quads + kv_quads ? 1 : 2;
-      head[u] = (quad - (kind[u] == 0 ? 0 : q_quads + (kind[u] - 1) * kv_quads)) * 4 + group;
-      if (quad >= min(quad0 + quads, all_quads) || head[u] >= (kind[u] == 0 ? p.H_q : p.H_kv)) head[u] = -1;
-      scale[u] = 1.f;
-      if (head[u] >= 0) {
-        const uint16_t *x = kind[u] == 0 ? p.q + t * p.q_token + (int64_t)head[u] * p.q_head
-                                         : (kind[u] == 1 ? p.k : p.v) + t * p.kv_token + (int64_t)head[u] * p.kv_head;
-        xa[u] = ld_v4(x + pa);
-        xb[u] = ld_v4(x + pb);
-        if (kE4m3 && kind[u] != 0) {
-          const float *scales = kind[u] == 1 ? p.c.k_scale : p.c.v_scale;
-          if (scales != nullptr) scale[u] = scales[head[u]];
-        }
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = unpack2(mul2(y[i], inv_scale));
+    w[i] = pack_e4m3x2(v.x, v.y);
+  }
+  return make_uint2(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+}
+
+constexpr int kTurnWarps = 4;
+constexpr int kTurnQuads = 2;       // groups of four rows whose loads are in flight at once
+constexpr int kTurnCtasPerSm = 8;
+enum { kTurnOnly = 0, kTurnAppend = 1, kTurnAppendE4m3 = 2 };
+
+// A warp takes one token's rows of one kind (queries, keys or values), or some groups of four of them: blockIdx.y says which,
+// blockIdx.x and the warp the token.  The rows are on their way while position and page are looked up.
+template <int kMode>
+__global__ void __launch_bounds__(kTurnWarps * 32, kTurnCtasPerSm)
+turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp, const int q_parts, const int kv_parts) {
+  const int lane = threadIdx.x & 31, piece = lane & 7, group = lane >> 3;
+  const int64_t t = (int64_t)blockIdx.x * kTurnWarps + (threadIdx.x >> 5);
+  const int part = blockIdx.y;
+  const int kind = kMode == kTurnOnly || part < q_parts ? 0 : part < q_parts + kv_parts ? 1 : 2;   // a query, a key, a value
+  const int first = (part - (kind == 0 ? 0 : kind == 1 ? q_parts : q_parts + kv_parts)) * per_warp * 4 + group;   // my first head
+  const int heads = kind == 0 ? p.H_q : p.H_kv, end = min(heads, first - group + per_warp * 4);
+  const int pa = first_piece(p.rope, piece) * 8, pab = second_piece(p.rope, piece) * 8 - pa;
+  // the frequencies through shared memory: lanes that ask the constant bank for 32 different words are served one by one
+  // (65536 tokens x 8 KV heads into an 8-bit cache 98.6 -> 9x us)
+  __shared__ uint64_t turns[kHeadDim / 2];
+  if (kind != 2 && threadIdx.x < kHeadDim / 2) turns[threadIdx.x] = p.rope.turns[threadIdx.x];
+  __syncthreads();
+  wait_for_predecessor();
+  if (t >= p.n_tokens) return;
+  const int64_t step = 4 * (kind == 0 ? p.q_head : p.kv_head);
+  const uint16_t *x = (kind == 0 ? p.q + t * p.q_token + first * p.q_head : (kind == 1 ? p.k : p.v) + t * p.kv_token + first * p.kv_head) + pa;
+  uint4 xa[kTurnQuads], xb[kTurnQuads];
+  auto load = [&](int h) {
+#pragma unroll
+    for (int u = 0; u < kTurnQuads; ++u)
+      if (h + 4 * u < end) {
+        xa[u] = ld_v4(x);
+        xb[u] = ld_v4(x + pab);
+        x += step;
       }
-    }
   };
-  load(quad0);                                                 // on their way while the page is looked up
-  if (position < 0) return;                                    // a place without a token
-  // the token's page: where any of position, sequence and page id is out of range its rows have no place
-  int page = -1, slot = 0;
-  bool in_table = seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size;
-  if (in_table) {
+  const int position = p.positions[t];
+  int64_t seq = t;
+  if (kMode != kTurnOnly && kind != 0 && p.seqs != nullptr) seq = p.seqs[t];
+  load(first);
+  if (kMode != kTurnOnly && position < 0) return;              // a place without a token
+  int page = -1, slot = 0;                                     // where any of position, sequence and page id is out of range: none
+  if (kMode != kTurnOnly && kind != 0 && seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size) {
     const int entry = page_of(position, p.c.page_size, p.c.page_magic);
     slot = position - entry * p.c.page_size;
     page = p.c.table[seq * p.c.table_stride + entry];
   }
   Angles a;
-  if (p.rope.rotary_dim > 0 && quad0 < q_quads + kv_quads) angles_of(p.rope, position, lane, a);
-  const int64_t row = paged_row(page, p.c.n_pages, slot, 0, p.c.page_stride, 0, p.c.token_stride);
-  if (row < 0 && lane == 0) atomicOr(p.c.status, kStatusBounds);
-  for (int q0 = quad0; q0 < min(quad0 + quads, all_quads); q0 += kRopeQuads) {
-    if (q0 > quad0) load(q0);
+  if (kind != 2 && p.rope.rotary_dim > 0) angles_of(turns, p.rope.amplitude, position, lane, a);
+  const bool as_is = kind == 2 || piece >= (p.rope.rotary_dim >> 4);   // none of this lane's pairs turns
+  if (kMode == kTurnAppendE4m3 && kind != 0) {
+    const int64_t row = paged_row(page, p.c.n_pages, slot, first, p.c.page_stride, p.c.head_stride, p.c.token_stride);
+    if (row < 0) {
+      if (lane == 0) atomicOr(p.c.status, kStatusBounds);
+      return;
+    }
+    uint8_t *o = (kind == 1 ? p.c.k : p.c.v) + row + pa;
+    const float *scales = kind == 1 ? p.c.k_scale : p.c.v_scale;
+    for (int h = first; h < end; h += 4 * kTurnQuads) {
+      if (h > first) load(h);
 #pragma unroll
-    for (int u = 0; u < kRopeQuads; ++u) {
-      if (head[u] < 0 || (kind[u] != 0 && row < 0)) continue;
-      float y[16];
-      const bool as_is = kind[u] == 2 || p.rope.rotary_dim == 0;
-      if (!as_is) rotate(p.rope, a, piece, xa[u], xb[u], y);
-      if (kind[u] == 0) {
-        uint16_t *o = p.q_out + t * p.q_out_token + (int64_t)head[u] * p.q_out_head;
-        st_v4(o + pa, as_is ? xa[u] : pack8_bf16(y));
-        st_v4(o + pb, as_is ? xb[u] : pack8_bf16(y + 8));
-        continue;
-      }
-      uint8_t *pages = kind[u] == 1 ? p.c.k : p.c.v;
-      const int64_t at = row + (int64_t)head[u] * p.c.head_stride;
-      if (kE4m3) {
-        if (as_is) {
+      for (int u = 0; u < kTurnQuads; ++u) {
+        if (h + 4 * u >= end) continue;
+        f32x2 y[8];
+        if (!as_is) {
+          rotate(p.rope, a, xa[u], xb[u], y);
+        } else {
           const uint32_t w[8] = {xa[u].x, xa[u].y, xa[u].z, xa[u].w, xb[u].x, xb[u].y, xb[u].z, xb[u].w};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) { y[2 * i] = bf16_low(w[i]); y[2 * i + 1] = bf16_high(w[i]); }
+          for (int i = 0; i < 8; ++i) y[i] = widen(w[i]);
         }
-        const float inv = 1.f / scale[u];
-        *reinterpret_cast<uint2 *>(pages + at + pa) = pack8_e4m3(y, inv);
-        *reinterpret_cast<uint2 *>(pages + at + pb) = pack8_e4m3(y + 8, inv);
-      } else {
-        uint16_t *o = reinterpret_cast<uint16_t *>(pages) + at;
-        st_v4(o + pa, as_is ? xa[u] : pack8_bf16(y));
-        st_v4(o + pb, as_is ? xb[u] : pack8_bf16(y + 8));
+        const float inv = scales != nullptr ? 1.f / scales[h + 4 * u] : 1.f;
+        *reinterpret_cast<uint2 *>(o) = pack8_e4m3(y, pack2(inv, inv));
+        *reinterpret_cast<uint2 *>(o + pab) = pack8_e4m3(y + 4, pack2(inv, inv));
+        o += 4 * p.c.head_stride;
+      }
+    }
+  } else {
+    uint16_t *o = p.q_out + t * p.q_out_token + first * p.q_out_head + pa;
+    int64_t o_step = 4 * p.q_out_head;
+    if (kMode != kTurnOnly && kind != 0) {
+      const int64_t row = paged_row(page, p.c.n_pages, slot, first, p.c.page_stride, p.c.head_stride, p.c.token_stride);
+      if (row < 0) {
+        if (lane == 0) atomicOr(p.c.status, kStatusBounds);
+        return;
+      }
+      o = reinterpret_cast<uint16_t *>(kind == 1 ? p.c.k : p.c.v) + row + pa;
+      o_step = 4 * p.c.head_stride;
+    }
+    for (int h = first; h < end; h += 4 * kTurnQuads) {
+      if (h > first) load(h);
+#pragma unroll
+      for (int u = 0; u < kTurnQuads; ++u) {
+        if (h + 4 * u >= end) continue;
+        if (as_is) {
+          st_v4(o, xa[u]);
+          st_v4(o + pab, xb[u]);
+        } else {
+          f32x2 y[8];
+          rotate(p.rope, a, xa[u], xb[u], y);
+          st_v4(o, pack8_bf16(y));
+          st_v4(o + pab, pack8_bf16(y + 4));
+        }
+        o += o_step;
       }
     }
   }
 }
 
-cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm, cudaStream_t stream) {
+// One group of four rows per warp where there are few (latency), up to all of a token's of a kind where those fill the device: they
+// share the angles.
+template <int kMode>
+static cudaError_t launch_turn(const PagedAppendParams &p, int n_sm, cudaStream_t stream) {
   if (p.n_tokens <= 0) return cudaSuccess;
-  const int all = (p.q != nullptr ? (p.H_q + 3) / 4 : 0) + 2 * ((p.H_kv + 3) / 4);
-  const int quads = quads_per_warp(p.n_tokens, all, n_sm), warps = (all + quads - 1) / quads;
-  const int64_t blocks = (p.n_tokens * warps + kRopeWarps - 1) / kRopeWarps;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_next(dtype == SAGEKV_CACHE_E4M3 ? paged_append_kernel<true> : paged_append_kernel<false>, dim3((unsigned)blocks),
-                     kRopeWarps * 32, 0, stream, 0, p, quads, warps);
+  const int q_quads = kMode == kTurnOnly || p.q != nullptr ? (p.H_q + 3) / 4 : 0, kv_quads = kMode == kTurnOnly ? 0 : (p.H_kv + 3) / 4;
+  const int64_t share = p.n_tokens * (q_quads + 2 * kv_quads) / ((int64_t)n_sm * kTurnWarps * kTurnCtasPerSm);
+  const int per_warp = (int)(share < 1 ? 1 : share > 8 ? 8 : share);
+  const int q_parts = (q_quads + per_warp - 1) / per_warp, kv_parts = (kv_quads + per_warp - 1) / per_warp;
+  if (q_parts + 2 * kv_parts > 65535) return cudaErrorInvalidValue;
+  return launch_next(turn_rows_kernel<kMode>, dim3((unsigned)((p.n_tokens + kTurnWarps - 1) / kTurnWarps), (unsigned)(q_parts + 2 * kv_parts)),
+                     kTurnWarps * 32, 0, stream, 0, p, per_warp, q_parts, kv_parts);
+}
+
+cudaError_t launch_rope(const PagedAppendParams &p, int n_sm, cudaStream_t stream) {
+  if (p.H_q <= 0) return cudaSuccess;
+  return launch_turn<kTurnOnly>(p, n_sm, stream);
+}
+
+cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm, cudaStream_t stream) {
+  return dtype == SAGEKV_CACHE_E4M3 ? launch_turn<kTurnAppendE4m3>(p, n_sm, stream) : launch_turn<kTurnAppend>(p, n_sm, stream);
 }
 
 // ---- compact ---------------------------------------------------------------------------------------------------------
 // Rows as in sagekv_select_compact: sink, the G lists, recent tokens, last token.  A warp takes up to 32 rows of one KV head:
 // each lane finds one row's place (list, then table: two loads one behind the other, for all rows at once), then the
-// rows are moved kCompactRows at a time, 16 bytes per lane, all loads ahead of the stores.  An 8-bit row is widened: code * scale,
-// rounded to bf16.
-constexpr int kCompactWarps = 8;
-constexpr int kCompactRows = 8;
+// rows are moved kRows at a time, 16 bytes per lane, all loads ahead of the stores.  An 8-bit row is widened: code * scale,
+// rounded to bf16.  Bound by that chain of loads where the rows are few, by their scatter where they are many.  (us, 8 heads x 2049 bf16
+// rows / 16 x 8193 bf16 / 16 x 8193 8-bit: eight rows at once in blocks of eight warps, loads past L1 5.25 / 35.9 / 24.9, four in blocks
+// of four 4.1 / 25.1 / 25.6, plain loads besides 3.5 / 24.0 / 25.5; eight at once and 32 per warp 3.7 / 25.2 / 23.3)
+constexpr int kCompactWarps = 4;
 
-template <bool kE4m3>
+template <bool kE4m3, int kRows>
 __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const PagedCompactParams p, const int rows_per_warp) {
   constexpr int kLanes = kE4m3 ? 8 : 16;                       // of a row of K or of V
   constexpr int kAtOnce = 32 / (2 * kLanes);                   // rows of K and V that a load instruction covers
-  constexpr int kLoads = kCompactRows / kAtOnce;
+  constexpr int kLoads = kRows / kAtOnce;
   const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1);
   const bool is_v = (lane / kLanes) & 1;
   const int sub = lane / (2 * kLanes);                         // which of the rows of a load
@@ -282,7 +299,7 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
   const float scale = kE4m3 && scales != nullptr ? scales[kvh] : 1.f;
   uint16_t *dst = (is_v ? p.Vc : p.Kc) + (int64_t)b * p.cs.batch_stride + (int64_t)kvh * p.cs.head_stride + (int64_t)first * p.cs.token_stride +
                   piece * (128 / kLanes);
-  for (int i0 = 0; i0 < n; i0 += kCompactRows) {
+  for (int i0 = 0; i0 < n; i0 += kRows) {
     uint4 row[kLoads];
     bool there[kLoads];
 #pragma unroll
@@ -290,7 +307,7 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
       const int i = i0 + u * kAtOnce + sub;
       const int64_t at = __shfl_sync(0xffffffffu, src, i & 31);
       there[u] = i < n && at >= 0;
-      if (there[u]) row[u] = ld_stream_v4(pages + at * (kE4m3 ? 1 : 2) + piece * 16);
+      if (there[u]) row[u] = ld_v4(pages + at * (kE4m3 ? 1 : 2) + piece * 16);
     }
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
@@ -316,12 +333,13 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
 
 cudaError_t launch_paged_compact(const PagedCompactParams &p, int dtype, int n_sm, cudaStream_t stream) {
   const int64_t L = p.S + (int64_t)p.G * p.k_q + p.R + 1, heads = (int64_t)p.B * p.H_kv;
-  // as many rows per warp as leave every SM a dozen warps
-  int rows = kCompactRows;
-  while (rows < 32 && L * heads / (2 * rows) >= (int64_t)n_sm * 12) rows *= 2;
+  // as many rows per warp as leave every SM two dozen warps
+  const bool e4m3 = dtype == SAGEKV_CACHE_E4M3;
+  int rows = 4;
+  while (rows < (e4m3 ? 32 : 8) && L * heads / (2 * rows) >= (int64_t)n_sm * 24) rows *= 2;
   const int64_t per_block = (int64_t)kCompactWarps * rows;
-  return launch_next(dtype == SAGEKV_CACHE_E4M3 ? paged_compact_kernel<true> : paged_compact_kernel<false>,
-                     dim3((unsigned)((L + per_block - 1) / per_block), (unsigned)heads), kCompactWarps * 32, 0, stream, 0, p, rows);
+  const auto kernel = !e4m3 ? paged_compact_kernel<false, 4> : rows >= 8 ? paged_compact_kernel<true, 8> : paged_compact_kernel<true, 4>;
+  return launch_next(kernel, dim3((unsigned)((L + per_block - 1) / per_block), (unsigned)heads), kCompactWarps * 32, 0, stream, 0, p, rows);
 }
 
 }  // namespace sagekv

@@ -10,11 +10,11 @@
 
 namespace sagekv {
 
-constexpr int kPsWarps = 6;
+constexpr int kPsWarps = 8;
 constexpr int kPsThreads = kPsWarps * 32;
-constexpr int kPsRingBytes = 2 * kSlotBytes;    // per warp: two stages of bf16 tiles, or four of 8-bit ones
+constexpr int kPsRingBytes = kSlotBytes;        // per warp: one stage of bf16 tiles, or two of 8-bit ones
 constexpr int kPsCtasPerSm = 3;
-constexpr int kPsMaxStages = 4;
+constexpr int kPsMaxStages = 2;
 constexpr int kPsMinUnits = 2;                  // a CTA's least share: two tiles per warp
 
 struct PsShared {
