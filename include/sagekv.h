@@ -517,7 +517,7 @@ int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sa
  *              tokens' queries, rotated beside in the same launch; q_out may
  *              be q (with the same strides).
  * Into a bf16 cache the (rotated) rows are rounded once; into an 8-bit cache the
- * fp32 values times the reciprocal of the scale are rounded once to the nearest e4m3
+ * fp32 values divided by the scale are rounded once to the nearest e4m3
  * value, those beyond +-448 (infinities too) to +-448, NaN to NaN.  seq_lens is neither read nor
  * changed.  No two tokens of a call may have the same sequence and position, or
  * reach the same row through shared pages: which of them a part of the row

@@ -396,6 +396,13 @@ def sagekv_decode_attn(ctx, q, k_new, v_new, Kc, Vc, state: CacheState, out, lse
         _check(code, "sagekv_decode_attn", ctx)
 
 
+_INT32 = torch.int32
+
+
+def _int32_row(t, n: int) -> bool:
+    return t.dtype is _INT32 and t.numel() == n and t.is_contiguous()
+
+
 class Layer:
     """Buffers of one layer's reduced cache (allocated with torch) plus the C state struct."""
 
@@ -492,36 +499,48 @@ class SageKV:
 
     def rope(self, x, positions, plan: RopePlan, out=None):
         """Rows x [tokens, heads, 128] rotated by their positions (int32 [tokens]); out may be x."""
+        shape = x.shape
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if positions.dtype != torch.int32 or positions.shape != x.shape[:1] or out.shape != x.shape:
-            raise ValueError("expected int32 positions, one per token, and out like x")
-        sagekv_rope(self.ctx, plan, x, x.shape[0], x.shape[1], positions, out)
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        elif out.shape != shape:
+            raise ValueError("expected out with the shape of x")
+        n, heads, _ = shape
+        if not _int32_row(positions, n):
+            raise ValueError("expected contiguous int32 positions, one per token")
+        sagekv_rope(self.ctx, plan, x, n, heads, positions, out)
         return out
 
     def paged_append(self, cache: PagedCache, k, v, positions, seqs=None, plan: RopePlan = None, q=None, q_out=None):
         """Keys and values [tokens, H_kv, 128] into their pages, keys (and queries q, into q_out) rotated by the plan.  Without
         seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
-        n = k.shape[0]
-        if positions.dtype != torch.int32 or positions.shape != (n,) or v.shape != k.shape or k.shape[1:] != (self.shape[1], 128):
-            raise ValueError("expected k and v [tokens, H_kv, 128] and int32 positions, one per token")
-        if seqs is not None and (seqs.dtype != torch.int32 or seqs.shape != (n,)):
-            raise ValueError("expected int32 seqs, one per token")
+        shape = k.shape
+        n, heads, _ = shape
+        if heads != self.shape[1] or v.shape != shape:
+            raise ValueError("expected k and v [tokens, H_kv, 128]")
+        if not _int32_row(positions, n) or not (seqs is None or _int32_row(seqs, n)):
+            raise ValueError("expected contiguous int32 positions and seqs, one per token")
         if q is not None:
+            shape = q.shape
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            if q.shape != (n, self.shape[0], 128) or q_out.shape != q.shape:
-                raise ValueError("expected q and q_out [tokens, H_q, 128]")
+                q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
+            elif q_out is not q and q_out.shape != shape:
+                raise ValueError("expected q_out with the shape of q")
+            if shape[0] != n or shape[1] != self.shape[0]:
+                raise ValueError("expected q [tokens, H_q, 128]")
         sagekv_paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
         return q_out
 
     def paged_attn(self, q, cache: PagedCache, out=None, lse=None):
         """Attention of one new token per sequence, q [>= n_seqs, H_q, 128], over its cache."""
+        shape, n = q.shape, cache.n_seqs
+        if shape[0] < n or shape[1] != self.shape[0]:
+            raise ValueError("expected q [n_seqs, H_q, 128]")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if q.shape[0] < cache.n_seqs or q.shape[1:] != (self.shape[0], 128) or q.stride(1) != 128 or out.shape[0] < cache.n_seqs or \
-                out.shape[1:] != q.shape[1:] or not out.is_contiguous() or (lse is not None and (lse.numel() < cache.n_seqs * self.shape[0] or not lse.is_contiguous())):
-            raise ValueError("expected q [n_seqs, H_q, 128] with its heads side by side, out like it and contiguous, lse [n_seqs, H_q]")
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        elif out.numel() < n * shape[1] * 128 or not out.is_contiguous():
+            raise ValueError("expected contiguous out [n_seqs, H_q, 128]")
+        if lse is not None and (lse.numel() < n * shape[1] or not lse.is_contiguous()):
+            raise ValueError("expected contiguous lse [n_seqs, H_q]")
         sagekv_paged_attn(self.ctx, q, cache, out, lse)
         return out
 

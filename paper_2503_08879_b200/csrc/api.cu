@@ -79,21 +79,21 @@ int sagekv_create(sagekv_ctx **out, const sagekv_shape *shape, int64_t max_ctx, 
   const size_t n_rows = (size_t)shape->batch * shape->n_q_heads;
   const size_t n_heads = (size_t)shape->batch * shape->n_kv_heads;
   cudaError_t e = cudaMalloc(&ctx->score_partials, n_rows * ctx->max_chunks * sizeof(float2));
-  if (e == cudaSuccess)
-    e = cudaMalloc(&ctx->decode_partials, n_heads * ctx->max_splits * kPartialStride * sizeof(float));
-  if (e == cudaSuccess) e = cudaMalloc(&ctx->tickets, (n_heads + 3) * sizeof(int32_t));
-  if (e == cudaSuccess) e = cudaMemset(ctx->tickets, 0, (n_heads + 3) * sizeof(int32_t));
-  if (e == cudaSuccess)
-    e = cudaMalloc(&ctx->paged_partials, (size_t)paged_attn_max_ctas(ctx->dev->n_sm) * 2 * kPartialStride * sizeof(float));
-  if (e == cudaSuccess) e = cudaMalloc(&ctx->paged_tickets, n_heads * sizeof(int32_t));
-  if (e == cudaSuccess) e = cudaMemset(ctx->paged_tickets, 0, n_heads * sizeof(int32_t));
-  if (e == cudaSuccess) ctx->status = ctx->tickets + n_heads + 1;
+  // (an allocation takes about 0.1 ms: the attention over pages has its scratch behind the decode step's)
+  const size_t decode_floats = n_heads * ctx->max_splits * kPartialStride;
+  const size_t paged_floats = (size_t)paged_attn_max_ctas(ctx->dev->n_sm) * 2 * kPartialStride;
+  if (e == cudaSuccess) e = cudaMalloc(&ctx->decode_partials, (decode_floats + paged_floats) * sizeof(float));
+  if (e == cudaSuccess) e = cudaMalloc(&ctx->tickets, (2 * n_heads + 3) * sizeof(int32_t));
+  if (e == cudaSuccess) e = cudaMemset(ctx->tickets, 0, (2 * n_heads + 3) * sizeof(int32_t));
+  if (e == cudaSuccess) {
+    ctx->status = ctx->tickets + n_heads + 1;
+    ctx->paged_tickets = ctx->tickets + n_heads + 3;
+    ctx->paged_partials = ctx->decode_partials + decode_floats;
+  }
   if (e != cudaSuccess) {
     cudaFree(ctx->score_partials);
     cudaFree(ctx->decode_partials);
     cudaFree(ctx->tickets);
-    cudaFree(ctx->paged_partials);
-    cudaFree(ctx->paged_tickets);
     delete ctx;
     cudaGetLastError();
     return e == cudaErrorMemoryAllocation ? SAGEKV_ERR_NOMEM : SAGEKV_ERR_CUDA;
@@ -107,8 +107,6 @@ int sagekv_destroy(sagekv_ctx *ctx) {
   cudaFree(ctx->score_partials);
   cudaFree(ctx->decode_partials);
   cudaFree(ctx->tickets);
-  cudaFree(ctx->paged_partials);
-  cudaFree(ctx->paged_tickets);
   delete ctx;
   return SAGEKV_OK;
 }

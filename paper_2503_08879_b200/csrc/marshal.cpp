@@ -277,6 +277,10 @@ PyObject *paged_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!count(n, 5) || !context(a[0], &ctx) || !pointer(a[1], &q) || !rows(a[1], &qs) || !cache.get(a[2], "PagedCache") || !pointer(a[3], &out) ||
       !pointer(a[4], &lse) || !current_stream(&stream))
     return nullptr;
+  if (q != nullptr && qs.head_stride != 128) {
+    PyErr_SetString(PyExc_ValueError, "expected queries whose heads lie side by side");
+    return nullptr;
+  }
   return answer([&] { return g_paged_attn(ctx, q, qs.token_stride, cache.p, out, static_cast<float *>(lse), stream); });
 }
 

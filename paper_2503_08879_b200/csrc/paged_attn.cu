@@ -30,9 +30,8 @@ constexpr int kPaThreads = kPaWarps * 32;
 constexpr int kPaRingBytes = 2 * kSlotBytes;        // per warp: one stage of bf16 tiles, or two of 8-bit ones
 constexpr int kPaHeadStride = kHeadDim + 4;         // floats between the heads of a warp's result: the 32 lanes of a store fall into 32 banks
 constexpr int kPaPairCost = 2;                      // places of the list in front of a pair's units: what a change of pair costs a CTA, in units
-constexpr int kPaMinPlaces = 2;                     // a CTA's least share of the list
+constexpr int kPaWholeUnits = 2;                    // pairs that are this short in the mean are not cut where there are CTAs to spare
 constexpr int kPaMaxStages = 2;
-constexpr int kPaJoin = 16;                         // parts of a shared pair that the last CTA reads at once
 
 struct PaShared {
   unsigned char ring[kPaWarps][kPaRingBytes];           // boxes with the 128-byte swizzle: 1024-byte boundaries
@@ -84,6 +83,60 @@ struct PaCursor {
 // places in the list that the pairs of a sequence take, per head
 __device__ __forceinline__ int places_of(int len) { return len > 0 ? (len + 16 * kPaWarps - 1) / (16 * kPaWarps) + kPaPairCost : 0; }
 
+// Joins the parts warp, warp + kPaWarps, ... of a shared pair (the first in slot 1 of its CTA, the others in slot 0 of theirs), kParts of
+// up to kHeads heads at a time with all their loads in flight; the result goes where a warp's result of tiles does.
+// (us from the last ticket to the end, 8 / 29 / 37 parts of four heads: a thread per four columns of a head going through
+// sixteen parts at a time 1.7 / 3.1 / 3.7, this 1.3 / 1.5 / 1.6)
+template <int kParts, int kHeads>
+__device__ __forceinline__ void join_parts(const float *first, int parts, int G, int warp, int lane, float *o_to, float2 *ml_to) {
+  static_assert(kParts * kHeads <= 32 && (kHeads & (kHeads - 1)) == 0, "a lane per part and head");
+  const int u_mine = lane / kHeads, h_mine = lane & (kHeads - 1);   // the lane of part u and head h works out its weight
+  float M = -INFINITY, l = 0.f;                              // of head h_mine
+  float4 o[kHeads];
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto part_of = [&](int i) { return i == 0 ? first : first + ((int64_t)i * 2 - 1) * kPartialStride; };
+  for (int i0 = warp; i0 < parts; i0 += kPaWarps * kParts) {
+    float2 ml = make_float2(-INFINITY, 0.f);
+    const int i_mine = i0 + u_mine * kPaWarps;
+    if (u_mine < kParts && i_mine < parts && h_mine < G)
+      ml = __ldcg(reinterpret_cast<const float2 *>(part_of(i_mine) + kMaxGroup * kHeadDim + 2 * h_mine));
+    float4 v[kParts][kHeads];
+#pragma unroll
+    for (int u = 0; u < kParts; ++u) {
+      const float *from = part_of(i0 + u * kPaWarps) + lane * 4;
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        v[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i0 + u * kPaWarps < parts && h < G) v[u][h] = __ldcg(reinterpret_cast<const float4 *>(from + h * kHeadDim));
+      }
+    }
+    float top = fmaxf(M, ml.x);
+#pragma unroll
+    for (int x = kHeads; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    const float f = ml.x == top ? 1.f : fast_exp2(ml.x - top), back = M == top ? 1.f : fast_exp2(M - top);   // (equal also where both are infinite)
+    float sum = ml.y * f;
+#pragma unroll
+    for (int x = kHeads; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+    l = l * back + sum;
+    M = top;
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      const float bk = __shfl_sync(0xffffffffu, back, h);
+      o[h].x *= bk; o[h].y *= bk; o[h].z *= bk; o[h].w *= bk;
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        const float fu = __shfl_sync(0xffffffffu, f, u * kHeads + h);
+        o[h].x += v[u][h].x * fu; o[h].y += v[u][h].y * fu; o[h].z += v[u][h].z * fu; o[h].w += v[u][h].w * fu;
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h)
+    if (h < G) *reinterpret_cast<float4 *>(o_to + h * kPaHeadStride + lane * 4) = o[h];
+  if (lane < G) ml_to[lane] = make_float2(M, l);
+}
+
 template <bool kE4m3>
 __global__ void __launch_bounds__(kPaThreads, kPagedCtasPerSm)
 paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -119,9 +172,9 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
   const int most_tokens = p.c.max_pages * p.c.page_size;
   const uint32_t n_ctas = gridDim.x;
   uint32_t total, per_cta, lo;
-  auto cut = [&] {                                           // (all fits 31 bits: the host has checked the most the tables can hold)
+  auto cut = [&](uint32_t least) {                           // (all fits 31 bits: the host has checked the most the tables can hold)
     const uint32_t all = total * (uint32_t)p.H_kv;
-    per_cta = max(all > 0u ? (all - 1u) / n_ctas + 1u : 0u, (uint32_t)kPaMinPlaces);
+    per_cta = max(all > 0u ? (all - 1u) / n_ctas + 1u : 0u, least);
     lo = min((uint32_t)blockIdx.x * per_cta, all);
     return (int)min(per_cta, all - lo);
   };
@@ -140,7 +193,10 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       if (lane >= o) incl += v;
     }
     total = (uint32_t)__shfl_sync(0xffffffffu, incl, 31);
-    n = cut();
+    // A second CTA per pair costs a ticket and the join, 2.4 us, and saves half of the steps of 1 us (8 heads x 100 tokens 4.9 / 5.9 us
+    // whole / cut, x 300 tokens 6.9 / 5.9).
+    constexpr uint32_t kWhole = kPaPairCost + kPaWholeUnits;
+    n = cut(total <= kWhole * (uint32_t)__popc(__ballot_sync(0xffffffffu, mine > 0)) ? kWhole : 1u);
     if (n > 0) {
       start_seq = __ffs(__ballot_sync(0xffffffffu, lo < (uint32_t)incl * p.H_kv)) - 1;
       start_before = __shfl_sync(0xffffffffu, incl - mine, start_seq) * p.H_kv;
@@ -170,7 +226,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       if (w < warp) before += warp_total[w];
       total += (uint32_t)warp_total[w];
     }
-    n = cut();
+    n = cut(1u);
     if (lo >= (uint32_t)before * p.H_kv && lo < (uint32_t)(before + mine) * p.H_kv) {   // the range begins in one of this thread's sequences
       int at = before, s = s0;
       for (int t; at + (t = places_of(tokens_of(p.c, s))) <= (int)(lo / p.H_kv); ++s) at += t;
@@ -381,75 +437,46 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       };
       // of a shared pair: slot 0 of a CTA whose range begins inside the pair, slot 1 of the one where the pair begins
       float *part = p.partials + ((int64_t)blockIdx.x * 2 + (cta_first == (int)blockIdx.x ? 1 : 0)) * kPartialStride;
-      for (int item = tid; item < p.G * (kHeadDim / 4); item += kPaThreads) {
-        const int h = item >> 5, col = (item & 31) * 4;
-        float M = -INFINITY, l = 0.f;
+      // the warps' results (of tiles, or of parts) as one
+      auto merge_warps = [&](auto emit) {
+        for (int item = tid; item < p.G * (kHeadDim / 4); item += kPaThreads) {
+          const int h = item >> 5, col = (item & 31) * 4;
+          float M = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < kPaWarps; ++w) M = fmaxf(M, sh.ml[w][h].x);
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int w = 0; w < kPaWarps; ++w) M = fmaxf(M, sh.ml[w][h].x);
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kPaWarps; ++w) {
-          const float2 ml = sh.ml[w][h];
-          const float f = ml.x == M ? 1.f : fast_exp2(ml.x - M);   // (equal also where both are infinite)
-          const float4 v = *reinterpret_cast<const float4 *>(sh.o[w] + h * kPaHeadStride + col);
-          l += ml.y * f;
-          o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+          for (int w = 0; w < kPaWarps; ++w) {
+            const float2 ml = sh.ml[w][h];
+            const float f = ml.x == M ? 1.f : fast_exp2(ml.x - M);   // (equal also where both are infinite)
+            const float4 v = *reinterpret_cast<const float4 *>(sh.o[w] + h * kPaHeadStride + col);
+            l += ml.y * f;
+            o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+          }
+          emit(h, col, o, M, l);
         }
-        if (whole) {
-          finish(h, col, o, M, l);
-        } else {
+      };
+      if (whole) {
+        merge_warps(finish);
+      } else {
+        merge_warps([&](int h, int col, float4 o, float M, float l) {
           *reinterpret_cast<float4 *>(part + h * kHeadDim + col) = o;
           if (col == 0) *reinterpret_cast<float2 *>(part + kMaxGroup * kHeadDim + 2 * h) = make_float2(M, l);
-        }
-      }
-      SAGEKV_STAMP(6);
-      if (!whole) {
+        });
+        SAGEKV_STAMP(6);
         const int parts = cta_last - cta_first + 1;
-        int32_t *ticket = p.tickets + (int64_t)at.seq * p.H_kv + at.head;
         __syncthreads();
-        if (tid == 0) {
-          __threadfence();                                   // (behind the barrier it stands for the whole block)
-          sh.arrived = atomicAdd(ticket, 1);
-          __threadfence();
-        }
+        if (tid == 0)                                        // (behind the barrier its release stands for the whole block, and so does its acquire)
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(sh.arrived) : "l"(p.tickets + (int64_t)at.seq * p.H_kv + at.head) : "memory");
         __syncthreads();
         SAGEKV_STAMP(7);
         if (sh.arrived == parts - 1) {                       // every other part is in scratch
-          if (tid == 0) *ticket = 0;
+          if (tid == 0) p.tickets[(int64_t)at.seq * p.H_kv + at.head] = 0;
           const float *first = p.partials + ((int64_t)cta_first * 2 + 1) * kPartialStride;
-          for (int item = tid; item < p.G * (kHeadDim / 4); item += kPaThreads) {
-            const int h = item >> 5, col = (item & 31) * 4;
-            float M = -INFINITY, l = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int i0 = 0; i0 < parts; i0 += kPaJoin) {    // kPaJoin parts' loads in flight
-              float2 ml[kPaJoin];
-              float4 v[kPaJoin];
-#pragma unroll
-              for (int u = 0; u < kPaJoin; ++u) {
-                const int i = i0 + u;
-                const float *part = i == 0 ? first : first + ((int64_t)i * 2 - 1) * kPartialStride;
-                ml[u] = make_float2(-INFINITY, 0.f);
-                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i < parts) {
-                  ml[u] = __ldcg(reinterpret_cast<const float2 *>(part + kMaxGroup * kHeadDim + 2 * h));
-                  v[u] = __ldcg(reinterpret_cast<const float4 *>(part + h * kHeadDim + col));
-                }
-              }
-              float top = M;
-#pragma unroll
-              for (int u = 0; u < kPaJoin; ++u) top = fmaxf(top, ml[u].x);
-              const float back = M == top ? 1.f : fast_exp2(M - top);
-              l *= back; o.x *= back; o.y *= back; o.z *= back; o.w *= back;
-              M = top;
-#pragma unroll
-              for (int u = 0; u < kPaJoin; ++u) {
-                const float f = ml[u].x == M ? 1.f : fast_exp2(ml[u].x - M);
-                l += ml[u].y * f;
-                o.x += v[u].x * f; o.y += v[u].y * f; o.z += v[u].z * f; o.w += v[u].w * f;
-              }
-            }
-            finish(h, col, o, M, l);
-          }
+          if (p.G <= 4) join_parts<4, 4>(first, parts, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+          else join_parts<2, 8>(first, parts, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+          __syncthreads();
+          merge_warps(finish);
         }
       }
       SAGEKV_STAMP(8);
@@ -473,7 +500,7 @@ cudaError_t launch_paged_attn(const PagedAttnParams &p, int dtype, int n_sm, cud
   CUtensorMap map_k, map_v;
   if (!make_page_map(&map_k, p.c.k, p.c, p.H_kv, e4m3) || !make_page_map(&map_v, p.c.v, p.c, p.H_kv, e4m3)) return cudaErrorInvalidValue;
   const int64_t most_units = ((int64_t)p.c.max_pages * p.c.page_size + 16 * kPaWarps - 1) / (16 * kPaWarps);   // of a sequence that fills its table
-  int64_t ctas = (p.c.n_seqs * p.H_kv * (most_units + kPaPairCost) + kPaMinPlaces - 1) / kPaMinPlaces;
+  int64_t ctas = p.c.n_seqs * p.H_kv * (most_units + kPaPairCost);
   if (ctas > paged_attn_max_ctas(n_sm)) ctas = paged_attn_max_ctas(n_sm);
   if (ctas < 1) ctas = 1;
   return launch_next(e4m3 ? paged_attn_kernel<true> : paged_attn_kernel<false>, dim3((unsigned)ctas), kPaThreads, sizeof(PaShared), stream, 0,

@@ -17,7 +17,7 @@ namespace sagekv {
 // The angle.  position * f passes 10^5 radians, of which 32 bits keep no fraction worth having.  The host gives
 // f / (2 pi) as a 64-bit fraction of a revolution, so the integer product with the position, modulo 2^64, is the
 // fraction of a revolution exactly (within position * 2^-65), for positions up to 2^31 of either sign; its upper 32 bits go to
-// sincospi in half revolutions.
+// sincospi in half revolutions, and what its 24-bit argument cuts off of them is added to first order.
 
 __device__ __forceinline__ int first_piece(const RopeArgs &r, int p) {
   const int turning = r.rotary_dim >> 4;
@@ -65,9 +65,12 @@ __device__ __forceinline__ void angles_of(const uint64_t *turns, float amplitude
   for (int e = 0; e < 2; ++e) {
     const uint64_t revolutions = turns[8 * p + 2 * group + e] * (uint64_t)(int64_t)position;
     const int half = (int)(uint32_t)((revolutions + 0x80000000ull) >> 32);      // in 2^-31 half revolutions, signed
-    sincospif((float)half * 0x1p-31f, &sn[e], &cs[e]);
-    cs[e] *= amplitude;
-    sn[e] *= amplitude;
+    const float rounded = (float)half;                         // (up to 2^31, which no int holds: the difference is taken modulo 2^32)
+    const float rest = (float)(int)((uint32_t)half - (uint32_t)(int64_t)rounded) * (3.14159265f * 0x1p-31f);
+    float s, c;
+    sincospif(rounded * 0x1p-31f, &s, &c);
+    cs[e] = (c - rest * s) * amplitude;
+    sn[e] = (s + rest * c) * amplitude;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -114,11 +117,21 @@ __device__ __forceinline__ uint4 pack8_bf16(const f32x2 *y) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint2 pack8_e4m3(const f32x2 *y, f32x2 inv_scale) {
+// The reciprocal of a scale in two parts, rounded down and what that leaves (positive, if ever so small, so that an infinite
+// value times it is no NaN): a product with both has one rounding, as a division would.
+struct Reciprocal {
+  f32x2 high, low;
+  __device__ __forceinline__ explicit Reciprocal(float scale) {
+    const float h = __frcp_rd(scale), l = fmaxf(fmaf(-h, scale, 1.f) * h, 1.1754944e-38f);
+    high = pack2(h, h);
+    low = pack2(l, l);
+  }
+};
+__device__ __forceinline__ uint2 pack8_e4m3(const f32x2 *y, const Reciprocal &inv) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 v = unpack2(mul2(y[i], inv_scale));
+    const float2 v = unpack2(fma2(y[i], inv.high, mul2(y[i], inv.low)));
     w[i] = pack_e4m3x2(v.x, v.y);
   }
   return make_uint2(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
@@ -195,9 +208,9 @@ turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[i] = widen(w[i]);
         }
-        const float inv = scales != nullptr ? 1.f / scales[h + 4 * u] : 1.f;
-        *reinterpret_cast<uint2 *>(o) = pack8_e4m3(y, pack2(inv, inv));
-        *reinterpret_cast<uint2 *>(o + pab) = pack8_e4m3(y + 4, pack2(inv, inv));
+        const Reciprocal inv(scales != nullptr ? scales[h + 4 * u] : 1.f);
+        *reinterpret_cast<uint2 *>(o) = pack8_e4m3(y, inv);
+        *reinterpret_cast<uint2 *>(o + pab) = pack8_e4m3(y + 4, inv);
         o += 4 * p.c.head_stride;
       }
     }
