@@ -47,7 +47,8 @@ enum {
   SAGEKV_ERR_NOMEM = -5,       /* scratch allocation failed in sagekv_create             */
   SAGEKV_ERR_TOO_LARGE = -6,   /* problem exceeds the fixed scratch of sagekv_score_static */
   SAGEKV_ERR_TIMEOUT = -7,     /* sagekv_status: a bounded wait inside a kernel ran out  */
-  SAGEKV_ERR_BOUNDS = -8,      /* sagekv_status, checked build: an out-of-range index was skipped */
+  SAGEKV_ERR_BOUNDS = -8,      /* sagekv_status: a paged call skipped what its table, positions or lengths put out of range
+                                * (checked build: any call an out-of-range index) */
   SAGEKV_ERR_DEVICE = -9       /* the context was created on another device than the current one */
 };
 
@@ -344,7 +345,8 @@ int64_t sagekv_scores_row_stride(const sagekv_ctx *ctx, int64_t n_ctx, int32_t n
 /* Device-side status of the context.  The kernels never trap: a wait on a copy
  * that does not arrive within its (generous) bound, or, in a library built
  * with -DSAGEKV_CHECKS, a global-memory index outside the extent the call was
- * given (the access is skipped), sets a bit in one int32 of context-owned device
+ * given (the access is skipped; in every build where it is a paged call's block
+ * table, positions, lists or lengths), sets a bit in one int32 of context-owned device
  * memory and the kernel runs to its end.  This call copies that word to
  * *device_status (may be NULL), clears it, and returns sagekv_status_code() of
  * it.  It synchronises (a blocking 4-byte copy): call it after synchronising

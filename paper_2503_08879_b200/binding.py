@@ -101,7 +101,7 @@ class PagedCache(C.Structure):
             raise ValueError("expected all tensors of a cache on one device")
         ptr = lambda t: None if t is None else t.data_ptr()
         super().__init__(ptr(k_pages), ptr(v_pages), k_pages.stride(0), k_pages.stride(1), k_pages.stride(2), ptr(block_table),
-                         max(block_table.stride(0), max_pages), ptr(seq_lens), ptr(k_scale), ptr(v_scale), k_pages.shape[0],
+                         block_table.stride(0) if n_seqs > 1 else max_pages, ptr(seq_lens), ptr(k_scale), ptr(v_scale), k_pages.shape[0],
                          k_pages.shape[2], max_pages, n_seqs, CACHE_BF16 if k_pages.dtype == torch.bfloat16 else CACHE_E4M3)
 
 
@@ -546,6 +546,9 @@ class SageKV:
 
     def paged_score(self, q_last, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, scores=None):
         """score() on a paged cache whose sequences have n_ctx tokens each."""
+        Hq, _, d, batch = self.shape
+        if q_last.numel() != batch * Hq * d or not q_last.is_contiguous():
+            raise ValueError("expected contiguous q_last [B, H_q, 128]")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
         sagekv_paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
@@ -554,8 +557,9 @@ class SageKV:
     def paged_compact(self, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, layer: Layer = None):
         """The reduced cache from lists of offsets into the eviction region, int32 [B, H_q, k_q], as sagekv_select_topk writes
         them (layer.idx is not touched)."""
-        if idx is not None and (idx.dtype != torch.int32 or not idx.is_contiguous()):
-            raise ValueError("expected contiguous int32 lists")
+        k_q = max(0, min(k // self.G, n_ctx - 1 - n_init - n_recent))
+        if idx is not None and not _int32_row(idx, self.shape[3] * self.shape[0] * k_q):
+            raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)]")
         if layer is None:
             layer = self.new_layer(n_init, n_recent, k)
         sagekv_paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)

@@ -71,6 +71,7 @@ int sagekv_create(sagekv_ctx **out, const sagekv_shape *shape, int64_t max_ctx, 
   }
   ctx->device = dev;
   ctx->max_chunks = (int)((max_ctx + kScoreChunk - 1) / kScoreChunk);
+  if (ctx->max_chunks < kPagedScoreChunks && (int64_t)shape->batch * shape->n_q_heads <= 4096) ctx->max_chunks = kPagedScoreChunks;
   {
     int cs, resident, smem;
     decode_geometry(max_len, 0, 0, nullptr, 0, &ctx->max_splits, &cs, &resident, &smem);   // clusters per head at the largest L ...
@@ -459,7 +460,7 @@ const char *sagekv_strerror(int code) {
     case SAGEKV_ERR_NOMEM: return "out of memory";
     case SAGEKV_ERR_TOO_LARGE: return "problem larger than the fixed scratch array";
     case SAGEKV_ERR_TIMEOUT: return "a bounded wait inside a kernel ran out";
-    case SAGEKV_ERR_BOUNDS: return "checked build: an index outside its buffer was skipped";
+    case SAGEKV_ERR_BOUNDS: return "an index outside its buffer was skipped (a paged call's table, position or length; any, in the checked build)";
     case SAGEKV_ERR_DEVICE: return "the context belongs to another device than the current one";
     default: return "unknown error code";
   }

@@ -12,8 +12,8 @@ struct sagekv_ctx {
   int device;               // the device the context was created on; every call must find it current
   const sagekv::DeviceInfo *dev;    // that device's one-time set-up
   float scale;
-  float2 *score_partials;   // [B*H_q, ceil(max_ctx / kScoreChunk)]
-  int max_chunks;
+  float2 *score_partials;   // [B*H_q, max_chunks]
+  int max_chunks;           // ceil(max_ctx / kScoreChunk), or the CTAs per head that the scores of short paged sequences are spread over
   float *decode_partials;   // [B*H_kv, max_splits (clusters per head), kPartialStride]
   int max_splits;
   float *paged_partials;    // [grid of the paged attention][2][kPartialStride]: what a CTA leaves of heads that it shares (behind decode_partials)

@@ -73,6 +73,7 @@ struct PagedAppendParams {
 cudaError_t launch_rope(const PagedAppendParams &p, int n_sm, cudaStream_t stream);   // the queries alone (H_q of them; every position counts)
 cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm, cudaStream_t stream);
 
+constexpr int kPagedScoreChunks = 64;   // CTAs that a KV head's tokens may be dealt to, however few (where the rows are not too many for it)
 // p.K and p.ks are unused; p.n_chunks (at most max_chunks) is set here
 cudaError_t launch_paged_score(ScoreParams p, const PagedView &c, int dtype, int max_chunks, int n_sm, cudaStream_t stream);
 cudaError_t paged_score_setup();   // one-time function attributes, with the device current

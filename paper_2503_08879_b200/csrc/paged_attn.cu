@@ -431,6 +431,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       const int64_t row0 = (int64_t)at.seq * p.H_q + at.head * p.G;   // the pair's first row of out and lse
       const float v_scale = kE4m3 && p.c.v_scale != nullptr ? p.c.v_scale[at.head] : 1.f;
       auto finish = [&](int h, int col, float4 o, float M, float l) {
+        if (!SAGEKV_OK_INDEX(p.c.status, at.seq < p.c.n_seqs && (at.head + 1) * p.G <= p.H_q && h < p.G)) return;
         const float inv = l == 0.f ? 0.f : v_scale / l;
         *reinterpret_cast<uint2 *>(p.out + (row0 + h) * kHeadDim + col) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
         if (p.lse != nullptr && col == 0) p.lse[row0 + h] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;

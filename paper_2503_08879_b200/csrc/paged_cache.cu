@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
     for (int u = 0; u < kLoads; ++u) {
       const int i = i0 + u * kAtOnce + sub;
       const int64_t at = __shfl_sync(0xffffffffu, src, i & 31);
-      there[u] = i < n && at >= 0;
+      there[u] = i < n && at >= 0 && SAGEKV_OK_INDEX(p.c.status, first + i < L && b < p.B);
       if (there[u]) row[u] = ld_v4(pages + at * (kE4m3 ? 1 : 2) + piece * 16);
     }
 #pragma unroll

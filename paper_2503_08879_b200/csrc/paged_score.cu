@@ -15,7 +15,7 @@ constexpr int kPsThreads = kPsWarps * 32;
 constexpr int kPsRingBytes = kSlotBytes;        // per warp: one stage of bf16 tiles, or two of 8-bit ones
 constexpr int kPsCtasPerSm = 3;
 constexpr int kPsMaxStages = 2;
-constexpr int kPsMinUnits = 2;                  // a CTA's least share: two tiles per warp
+constexpr int kPsMinUnits = 1;                  // a CTA's least share: a tile per warp
 
 struct PsShared {
   unsigned char ring[kPsWarps][kPsRingBytes];   // boxes with the 128-byte swizzle: 1024-byte boundaries

@@ -96,6 +96,21 @@ def test_sharp_and_flat_weights(spread, scale, dtype):
     run(8, 2, [900, 33], dtype=dtype, spread=spread, softmax_scale=scale, want_lse=scale != 1e-9)
 
 
+def test_a_table_without_columns_and_one_of_a_wider_table():
+    B, sk = context(8, 2, 3)
+    pool = O.Pool(2, 16, 3, 6, BF16, "cuda").fill([90, 20, 64])
+    q = queries(pool, 3, 8)
+    none = B.PagedCache(pool.k, pool.v, pool.table[:, :0], torch.zeros(3, dtype=torch.int32, device="cuda"))
+    lse = torch.zeros(3, 8, device="cuda")
+    assert not sk.paged_attn(q, none, None, lse).any() and torch.all(lse == -math.inf) and sk.status() == 0
+    lens = [64, 20, 64]
+    some = B.PagedCache(pool.k, pool.v, pool.table[:, :4], torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    out = sk.paged_attn(q, some, None, lse)
+    check(pool, lens, q, out, lse)
+    assert sk.status() == 0
+    sk.close()
+
+
 def test_without_lse_and_with_strided_queries():
     B, sk = context(8, 2, 3)
     lens = [100, 0, 35]

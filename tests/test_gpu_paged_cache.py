@@ -524,8 +524,11 @@ def test_score_and_compact_refusals():
     B.sagekv_set_group_mode(sk.ctx, 1)
     assert code(idx, cache, N, 4, 10, 10, layer.Kc, layer.Vc) == B.ERR_UNSUPPORTED
     B.sagekv_set_group_mode(sk.ctx, 0)
+    for bad in (idx.long(), idx[:, :, :4], idx[:1].contiguous()):
+        with pytest.raises(ValueError):
+            sk.paged_compact(bad, cache, N, 4, 10, 10)
     with pytest.raises(ValueError):
-        sk.paged_compact(idx.long(), cache, N, 4, 10, 10)
+        sk.paged_score(q[:1], cache, N, 4, 10, scores)
     torch.cuda.synchronize()
     assert torch.all(layer.Kc == 7) and torch.all(scores == 7) and sk.status() == 0
     sk.close()

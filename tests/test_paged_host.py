@@ -100,6 +100,14 @@ def test_the_python_description_refuses_what_the_struct_cannot_say(B):
             B.PagedCache(*args)
 
 
+def test_rows_of_the_table_must_lie_apart(B):
+    """A row expanded to several sequences has stride 0: refused, and not taken for rows one behind the other."""
+    k = torch.zeros(4, 8, 16, 128, dtype=torch.bfloat16)
+    assert refusal(B, B.PagedCache(k, k, torch.zeros(1, 3, dtype=torch.int32).expand(3, 3))) == B.ERR_INVALID
+    B.sagekv_paged_check(shape(B), B.PagedCache(k, k, torch.zeros(1, 3, dtype=torch.int32).expand(1, 3)))
+    B.sagekv_paged_check(shape(B), B.PagedCache(k, k, torch.zeros(5, 9, dtype=torch.int32)[:3, :4]))
+
+
 @pytest.mark.parametrize("page_size", [16, 48, 64, 80, 1008, 65536])
 def test_offsets(B, page_size):
     """Addresses against a plain division, beyond 32 bits too; pages that are none have no address."""
