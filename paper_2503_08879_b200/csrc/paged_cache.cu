@@ -16,8 +16,8 @@ namespace sagekv {
 //
 // The angle.  position * f passes 10^5 radians, of which 32 bits keep no fraction worth having.  The host gives
 // f / (2 pi) as a 64-bit fraction of a revolution, so the integer product with the position, modulo 2^64, is the
-// fraction of a revolution exactly (within position * 2^-65), for positions up to 2^31 of either sign; its upper 32 bits go to
-// sincospi in half revolutions, and what its 24-bit argument cuts off of them is added to first order.
+// fraction of a revolution exactly (within position * 2^-65), for positions up to 2^31 of either sign; its upper 32 bits are
+// taken, and since the quadrant is two of them, no reduction of the argument is needed for sine and cosine.
 
 __device__ __forceinline__ int first_piece(const RopeArgs &r, int p) {
   const int turning = r.rotary_dim >> 4;
@@ -57,20 +57,48 @@ struct Angles {
   f32x2 cs[4], sn[4], ns[4];   // cosines, sines and negated sines of a lane's eight pairs
 };
 
+// Sines and cosines of two angles, given in 2^-31 half revolutions.  The upper two bits (rounded) are the quadrant, the rest is at
+// most an eighth of a revolution either way: there the Taylor series to the ninth and tenth power leave out less than 2e-9, and
+// the rest's rounding to 24 bits moves the angle by less than 3e-8.
+__device__ __forceinline__ void sines(int half0, int half1, float (&sn)[2], float (&cs)[2]) {
+  const int q[2] = {(int)((uint32_t)half0 + 0x20000000u) >> 30, (int)((uint32_t)half1 + 0x20000000u) >> 30};
+  const f32x2 pi = pack2(3.14159265f * 0x1p-31f, 3.14159265f * 0x1p-31f);
+  const f32x2 x = mul2(pack2((float)(int)((uint32_t)half0 - ((uint32_t)q[0] << 30)), (float)(int)((uint32_t)half1 - ((uint32_t)q[1] << 30))), pi);
+  const f32x2 z = mul2(x, x);
+  auto both = [](float v) { return pack2(v, v); };
+  f32x2 s = fma2(z, both(1.f / 362880.f), both(-1.f / 5040.f)), c = fma2(z, both(-1.f / 3628800.f), both(1.f / 40320.f));
+  s = fma2(z, s, both(1.f / 120.f));
+  c = fma2(z, c, both(-1.f / 720.f));
+  s = fma2(z, s, both(-1.f / 6.f));
+  c = fma2(z, c, both(1.f / 24.f));
+  s = fma2(mul2(z, s), x, x);
+  c = fma2(z, c, both(-0.5f));
+  c = fma2(z, c, both(1.f));
+  const float2 s2 = unpack2(s), c2 = unpack2(c);
+  const float ss[2] = {s2.x, s2.y}, cc[2] = {c2.x, c2.y};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {                                // a quadrant on: (cos, sin) becomes (-sin, cos)
+    const float a = q[e] & 1 ? cc[e] : ss[e], b = q[e] & 1 ? ss[e] : cc[e];
+    sn[e] = __uint_as_float(__float_as_uint(a) ^ ((uint32_t)(q[e] & 2) << 30));
+    cs[e] = __uint_as_float(__float_as_uint(b) ^ ((uint32_t)((q[e] + 1) & 2) << 30));
+  }
+}
+
 // lane: p = lane & 7, group = lane >> 3; all lanes take part
 __device__ __forceinline__ void angles_of(const uint64_t *turns, float amplitude, int position, int lane, Angles &a) {
   const int p = lane & 7, group = lane >> 3;
   float cs[2], sn[2];
+  int half[2];                                                 // in 2^-31 half revolutions, signed
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const uint64_t revolutions = turns[8 * p + 2 * group + e] * (uint64_t)(int64_t)position;
-    const int half = (int)(uint32_t)((revolutions + 0x80000000ull) >> 32);      // in 2^-31 half revolutions, signed
-    const float rounded = (float)half;                         // (up to 2^31, which no int holds: the difference is taken modulo 2^32)
-    const float rest = (float)(int)((uint32_t)half - (uint32_t)(int64_t)rounded) * (3.14159265f * 0x1p-31f);
-    float s, c;
-    sincospif(rounded * 0x1p-31f, &s, &c);
-    cs[e] = (c - rest * s) * amplitude;
-    sn[e] = (s + rest * c) * amplitude;
+    half[e] = (int)(uint32_t)((revolutions + 0x80000000ull) >> 32);
+  }
+  sines(half[0], half[1], sn, cs);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    sn[e] *= amplitude;
+    cs[e] *= amplitude;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -117,12 +145,16 @@ __device__ __forceinline__ uint4 pack8_bf16(const f32x2 *y) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// The reciprocal of a scale in two parts, rounded down and what that leaves (positive, if ever so small, so that an infinite
-// value times it is no NaN): a product with both has one rounding, as a division would.
+// The reciprocal of a scale in two parts: one a little below it (by 2^-22, more than the approximation is off), and what that leaves,
+// which is therefore positive (an infinite value times both is infinite, and no NaN): a product with both has one
+// rounding, as a division would.
 struct Reciprocal {
   f32x2 high, low;
   __device__ __forceinline__ explicit Reciprocal(float scale) {
-    const float h = __frcp_rd(scale), l = fmaxf(fmaf(-h, scale, 1.f) * h, 1.1754944e-38f);
+    float h;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(h) : "f"(scale));
+    h *= 1.f - 0x1p-22f;
+    const float l = fmaf(-h, scale, 1.f) * h;
     high = pack2(h, h);
     low = pack2(l, l);
   }
@@ -139,108 +171,107 @@ __device__ __forceinline__ uint2 pack8_e4m3(const f32x2 *y, const Reciprocal &in
 
 constexpr int kTurnWarps = 4;
 constexpr int kTurnQuads = 2;       // groups of four rows whose loads are in flight at once
-constexpr int kTurnCtasPerSm = 8;
+constexpr int kTurnCtasPerSm = 7;
+constexpr int kTurnWaves = 4;       // waves of blocks that are left to even out
 enum { kTurnOnly = 0, kTurnAppend = 1, kTurnAppendE4m3 = 2 };
 
-// A warp takes one token's rows of one kind (queries, keys or values), or some groups of four of them: blockIdx.y says which,
-// blockIdx.x and the warp the token.  The rows are on their way while position and page are looked up.
+// A warp takes rows of one kind (queries, keys or values; all of a token's, or some groups of four of them: blockIdx.y says which) of
+// one token after another.  The rows are on their way while position and page are looked up.
 template <int kMode>
 __global__ void __launch_bounds__(kTurnWarps * 32, kTurnCtasPerSm)
 turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp, const int q_parts, const int kv_parts) {
   const int lane = threadIdx.x & 31, piece = lane & 7, group = lane >> 3;
-  const int64_t t = (int64_t)blockIdx.x * kTurnWarps + (threadIdx.x >> 5);
   const int part = blockIdx.y;
   const int kind = kMode == kTurnOnly || part < q_parts ? 0 : part < q_parts + kv_parts ? 1 : 2;   // a query, a key, a value
   const int first = (part - (kind == 0 ? 0 : kind == 1 ? q_parts : q_parts + kv_parts)) * per_warp * 4 + group;   // my first head
   const int heads = kind == 0 ? p.H_q : p.H_kv, end = min(heads, first - group + per_warp * 4);
   const int pa = first_piece(p.rope, piece) * 8, pab = second_piece(p.rope, piece) * 8 - pa;
+  const bool as_is = kind == 2 || piece >= (p.rope.rotary_dim >> 4);   // none of this lane's pairs turns
   // the frequencies through shared memory: lanes that ask the constant bank for 32 different words are served one by one
-  // (65536 tokens x 8 KV heads into an 8-bit cache 98.6 -> 9x us)
+  // (65536 tokens x 8 KV heads into an 8-bit cache 98.6 -> 84.1 us)
   __shared__ uint64_t turns[kHeadDim / 2];
   if (kind != 2 && threadIdx.x < kHeadDim / 2) turns[threadIdx.x] = p.rope.turns[threadIdx.x];
   __syncthreads();
   wait_for_predecessor();
-  if (t >= p.n_tokens) return;
-  const int64_t step = 4 * (kind == 0 ? p.q_head : p.kv_head);
-  const uint16_t *x = (kind == 0 ? p.q + t * p.q_token + first * p.q_head : (kind == 1 ? p.k : p.v) + t * p.kv_token + first * p.kv_head) + pa;
-  uint4 xa[kTurnQuads], xb[kTurnQuads];
-  auto load = [&](int h) {
+  const int64_t from_step = 4 * (kind == 0 ? p.q_head : p.kv_head), from_token = kind == 0 ? p.q_token : p.kv_token;
+  const uint16_t *from = (kind == 0 ? p.q + first * p.q_head : (kind == 1 ? p.k : p.v) + first * p.kv_head) + pa;
+  const int64_t stride = (int64_t)gridDim.x * kTurnWarps;
+  int64_t t = (int64_t)blockIdx.x * kTurnWarps + (threadIdx.x >> 5);
+  auto sequence_of = [&](int64_t token) { return kMode != kTurnOnly && kind != 0 && p.seqs != nullptr ? p.seqs[token] : (int)token; };
+  int next_position = t < p.n_tokens ? p.positions[t] : -1, next_seq = t < p.n_tokens ? sequence_of(t) : -1;
+  for (; t < p.n_tokens; t += stride) {
+    const uint16_t *x = from + t * from_token;
+    uint4 xa[kTurnQuads], xb[kTurnQuads];
+    auto load = [&](int h) {
 #pragma unroll
-    for (int u = 0; u < kTurnQuads; ++u)
-      if (h + 4 * u < end) {
-        xa[u] = ld_v4(x);
-        xb[u] = ld_v4(x + pab);
-        x += step;
-      }
-  };
-  const int position = p.positions[t];
-  int64_t seq = t;
-  if (kMode != kTurnOnly && kind != 0 && p.seqs != nullptr) seq = p.seqs[t];
-  load(first);
-  if (kMode != kTurnOnly && position < 0) return;              // a place without a token
-  int page = -1, slot = 0;                                     // where any of position, sequence and page id is out of range: none
-  if (kMode != kTurnOnly && kind != 0 && seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size) {
-    const int entry = page_of(position, p.c.page_size, p.c.page_magic);
-    slot = position - entry * p.c.page_size;
-    page = p.c.table[seq * p.c.table_stride + entry];
-  }
-  Angles a;
-  if (kind != 2 && p.rope.rotary_dim > 0) angles_of(turns, p.rope.amplitude, position, lane, a);
-  const bool as_is = kind == 2 || piece >= (p.rope.rotary_dim >> 4);   // none of this lane's pairs turns
-  if (kMode == kTurnAppendE4m3 && kind != 0) {
-    const int64_t row = paged_row(page, p.c.n_pages, slot, first, p.c.page_stride, p.c.head_stride, p.c.token_stride);
-    if (row < 0) {
+      for (int u = 0; u < kTurnQuads; ++u)
+        if (h + 4 * u < end) {
+          xa[u] = ld_v4(x);
+          xb[u] = ld_v4(x + pab);
+          x += from_step;
+        }
+    };
+    load(first);
+    const int position = next_position, seq = next_seq;
+    if (t + stride < p.n_tokens) {
+      next_position = p.positions[t + stride];
+      next_seq = sequence_of(t + stride);
+    }
+    if (kMode != kTurnOnly && position < 0) continue;          // a place without a token
+    int64_t row = -1;                                          // where any of position, sequence and page id is out of range: none
+    if (kMode != kTurnOnly && kind != 0 && seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size) {
+      const int entry = page_of(position, p.c.page_size, p.c.page_magic);
+      row = paged_row(p.c.table[seq * p.c.table_stride + entry], p.c.n_pages, position - entry * p.c.page_size, first, p.c.page_stride,
+                      p.c.head_stride, p.c.token_stride);
+    }
+    Angles a;
+    if (kind != 2 && p.rope.rotary_dim > 0) angles_of(turns, p.rope.amplitude, position, lane, a);
+    if (kMode != kTurnOnly && kind != 0 && row < 0) {
       if (lane == 0) atomicOr(p.c.status, kStatusBounds);
-      return;
+      continue;
     }
-    uint8_t *o = (kind == 1 ? p.c.k : p.c.v) + row + pa;
-    const float *scales = kind == 1 ? p.c.k_scale : p.c.v_scale;
-    for (int h = first; h < end; h += 4 * kTurnQuads) {
-      if (h > first) load(h);
+    if (kMode == kTurnAppendE4m3 && kind != 0) {
+      uint8_t *o = (kind == 1 ? p.c.k : p.c.v) + row + pa;
+      const float *scales = kind == 1 ? p.c.k_scale : p.c.v_scale;
+      for (int h = first; h < end; h += 4 * kTurnQuads) {
+        if (h > first) load(h);
 #pragma unroll
-      for (int u = 0; u < kTurnQuads; ++u) {
-        if (h + 4 * u >= end) continue;
-        f32x2 y[8];
-        if (!as_is) {
-          rotate(p.rope, a, xa[u], xb[u], y);
-        } else {
-          const uint32_t w[8] = {xa[u].x, xa[u].y, xa[u].z, xa[u].w, xb[u].x, xb[u].y, xb[u].z, xb[u].w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = widen(w[i]);
-        }
-        const Reciprocal inv(scales != nullptr ? scales[h + 4 * u] : 1.f);
-        *reinterpret_cast<uint2 *>(o) = pack8_e4m3(y, inv);
-        *reinterpret_cast<uint2 *>(o + pab) = pack8_e4m3(y + 4, inv);
-        o += 4 * p.c.head_stride;
-      }
-    }
-  } else {
-    uint16_t *o = p.q_out + t * p.q_out_token + first * p.q_out_head + pa;
-    int64_t o_step = 4 * p.q_out_head;
-    if (kMode != kTurnOnly && kind != 0) {
-      const int64_t row = paged_row(page, p.c.n_pages, slot, first, p.c.page_stride, p.c.head_stride, p.c.token_stride);
-      if (row < 0) {
-        if (lane == 0) atomicOr(p.c.status, kStatusBounds);
-        return;
-      }
-      o = reinterpret_cast<uint16_t *>(kind == 1 ? p.c.k : p.c.v) + row + pa;
-      o_step = 4 * p.c.head_stride;
-    }
-    for (int h = first; h < end; h += 4 * kTurnQuads) {
-      if (h > first) load(h);
-#pragma unroll
-      for (int u = 0; u < kTurnQuads; ++u) {
-        if (h + 4 * u >= end) continue;
-        if (as_is) {
-          st_v4(o, xa[u]);
-          st_v4(o + pab, xb[u]);
-        } else {
+        for (int u = 0; u < kTurnQuads; ++u) {
+          if (h + 4 * u >= end) continue;
           f32x2 y[8];
-          rotate(p.rope, a, xa[u], xb[u], y);
-          st_v4(o, pack8_bf16(y));
-          st_v4(o + pab, pack8_bf16(y + 4));
+          if (!as_is) {
+            rotate(p.rope, a, xa[u], xb[u], y);
+          } else {
+            const uint32_t w[8] = {xa[u].x, xa[u].y, xa[u].z, xa[u].w, xb[u].x, xb[u].y, xb[u].z, xb[u].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = widen(w[i]);
+          }
+          const Reciprocal inv(scales != nullptr ? scales[h + 4 * u] : 1.f);
+          *reinterpret_cast<uint2 *>(o) = pack8_e4m3(y, inv);
+          *reinterpret_cast<uint2 *>(o + pab) = pack8_e4m3(y + 4, inv);
+          o += 4 * p.c.head_stride;
         }
-        o += o_step;
+      }
+    } else {
+      uint16_t *o = kMode == kTurnOnly || kind == 0 ? p.q_out + t * p.q_out_token + first * p.q_out_head + pa
+                                                    : reinterpret_cast<uint16_t *>(kind == 1 ? p.c.k : p.c.v) + row + pa;
+      const int64_t o_step = 4 * (kMode == kTurnOnly || kind == 0 ? p.q_out_head : p.c.head_stride);
+      for (int h = first; h < end; h += 4 * kTurnQuads) {
+        if (h > first) load(h);
+#pragma unroll
+        for (int u = 0; u < kTurnQuads; ++u) {
+          if (h + 4 * u >= end) continue;
+          if (as_is) {
+            st_v4(o, xa[u]);
+            st_v4(o + pab, xb[u]);
+          } else {
+            f32x2 y[8];
+            rotate(p.rope, a, xa[u], xb[u], y);
+            st_v4(o, pack8_bf16(y));
+            st_v4(o + pab, pack8_bf16(y + 4));
+          }
+          o += o_step;
+        }
       }
     }
   }
@@ -252,12 +283,15 @@ template <int kMode>
 static cudaError_t launch_turn(const PagedAppendParams &p, int n_sm, cudaStream_t stream) {
   if (p.n_tokens <= 0) return cudaSuccess;
   const int q_quads = kMode == kTurnOnly || p.q != nullptr ? (p.H_q + 3) / 4 : 0, kv_quads = kMode == kTurnOnly ? 0 : (p.H_kv + 3) / 4;
-  const int64_t share = p.n_tokens * (q_quads + 2 * kv_quads) / ((int64_t)n_sm * kTurnWarps * kTurnCtasPerSm);
+  const int64_t warps = (int64_t)n_sm * kTurnWarps * kTurnCtasPerSm;   // that run at once
+  const int64_t share = p.n_tokens * (q_quads + 2 * kv_quads) / warps;
   const int per_warp = (int)(share < 1 ? 1 : share > 8 ? 8 : share);
-  const int q_parts = (q_quads + per_warp - 1) / per_warp, kv_parts = (kv_quads + per_warp - 1) / per_warp;
-  if (q_parts + 2 * kv_parts > 65535) return cudaErrorInvalidValue;
-  return launch_next(turn_rows_kernel<kMode>, dim3((unsigned)((p.n_tokens + kTurnWarps - 1) / kTurnWarps), (unsigned)(q_parts + 2 * kv_parts)),
-                     kTurnWarps * 32, 0, stream, 0, p, per_warp, q_parts, kv_parts);
+  const int q_parts = (q_quads + per_warp - 1) / per_warp, kv_parts = (kv_quads + per_warp - 1) / per_warp, parts = q_parts + 2 * kv_parts;
+  if (parts > 65535) return cudaErrorInvalidValue;
+  const int64_t rounds = p.n_tokens * parts / (kTurnWaves * warps);    // tokens of a warp, if kTurnWaves waves of blocks are to remain
+  const int64_t tokens = (p.n_tokens + (rounds > 1 ? rounds : 1) - 1) / (rounds > 1 ? rounds : 1);
+  return launch_next(turn_rows_kernel<kMode>, dim3((unsigned)((tokens + kTurnWarps - 1) / kTurnWarps), (unsigned)parts), kTurnWarps * 32, 0,
+                     stream, 0, p, per_warp, q_parts, kv_parts);
 }
 
 cudaError_t launch_rope(const PagedAppendParams &p, int n_sm, cudaStream_t stream) {
