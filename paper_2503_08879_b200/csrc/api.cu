@@ -80,9 +80,9 @@ int sagekv_create(sagekv_ctx **out, const sagekv_shape *shape, int64_t max_ctx, 
   const size_t n_rows = (size_t)shape->batch * shape->n_q_heads;
   const size_t n_heads = (size_t)shape->batch * shape->n_kv_heads;
   cudaError_t e = cudaMalloc(&ctx->score_partials, n_rows * ctx->max_chunks * sizeof(float2));
-  // (an allocation takes about 0.1 ms: the attention over pages has its scratch behind the decode step's)
+  // (the attention over pages has its scratch behind the decode step's)
   const size_t decode_floats = n_heads * ctx->max_splits * kPartialStride;
-  const size_t paged_floats = (size_t)paged_attn_max_ctas(ctx->dev->n_sm) * 2 * kPartialStride;
+  const size_t paged_floats = (size_t)paged_attn_max_ctas(ctx->dev->n_sm) * 2 * paged_part_floats(ctx->G);
   if (e == cudaSuccess) e = cudaMalloc(&ctx->decode_partials, (decode_floats + paged_floats) * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&ctx->tickets, (2 * n_heads + 3) * sizeof(int32_t));
   if (e == cudaSuccess) e = cudaMemset(ctx->tickets, 0, (2 * n_heads + 3) * sizeof(int32_t));

@@ -16,7 +16,7 @@ struct sagekv_ctx {
   int max_chunks;           // ceil(max_ctx / kScoreChunk), or the CTAs per head that the scores of short paged sequences are spread over
   float *decode_partials;   // [B*H_kv, max_splits (clusters per head), kPartialStride]
   int max_splits;
-  float *paged_partials;    // [grid of the paged attention][2][kPartialStride]: what a CTA leaves of heads that it shares (behind decode_partials)
+  float *paged_partials;    // [grid of the paged attention][2][paged_part_floats(G)]: what a CTA leaves of heads that it shares (behind decode_partials)
   int32_t *paged_tickets;   // [B*H_kv] arrival counters of the paged attention, zero between launches (behind tickets)
   int32_t *tickets;         // [B*H_kv + 1], zero between launches; the status word and the selection's ready word follow them
   int32_t *status;          // one int32: kStatus* bits raised by the kernels

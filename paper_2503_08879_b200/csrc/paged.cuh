@@ -39,6 +39,7 @@ __host__ __device__ inline int64_t paged_row(int page, int n_pages, int slot, in
 // ---- attention of one token per sequence over its pages -------------------------------------------------------
 constexpr int kPagedCtasPerSm = 2;
 constexpr int paged_attn_max_ctas(int n_sm) { return kPagedCtasPerSm * n_sm; }
+__host__ __device__ constexpr int paged_part_floats(int G) { return G * kHeadDim + (2 * G + 3) / 4 * 4; }   // what a CTA leaves of a pair: O[G][128], (m, l)[G]
 
 struct PagedAttnParams {
   PagedView c;
@@ -46,7 +47,7 @@ struct PagedAttnParams {
   int64_t q_stride;
   uint16_t *out;           // [n_seqs, H_q, 128]
   float *lse;              // [n_seqs, H_q] or null
-  float *partials;         // [CTAs][2][kPartialStride]
+  float *partials;         // [CTAs][2][paged_part_floats(G)]
   int32_t *tickets;        // [n_seqs * H_kv], zero between launches
   int G, H_q, H_kv;
   float scale_log2;

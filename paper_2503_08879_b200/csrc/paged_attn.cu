@@ -95,12 +95,13 @@ __device__ __forceinline__ void join_parts(const float *first, int parts, int G,
   float4 o[kHeads];
 #pragma unroll
   for (int h = 0; h < kHeads; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto part_of = [&](int i) { return i == 0 ? first : first + ((int64_t)i * 2 - 1) * kPartialStride; };
+  const int part_floats = paged_part_floats(G);
+  auto part_of = [&](int i) { return i == 0 ? first : first + ((int64_t)i * 2 - 1) * part_floats; };
   for (int i0 = warp; i0 < parts; i0 += kPaWarps * kParts) {
     float2 ml = make_float2(-INFINITY, 0.f);
     const int i_mine = i0 + u_mine * kPaWarps;
     if (u_mine < kParts && i_mine < parts && h_mine < G)
-      ml = __ldcg(reinterpret_cast<const float2 *>(part_of(i_mine) + kMaxGroup * kHeadDim + 2 * h_mine));
+      ml = __ldcg(reinterpret_cast<const float2 *>(part_of(i_mine) + G * kHeadDim + 2 * h_mine));
     float4 v[kParts][kHeads];
 #pragma unroll
     for (int u = 0; u < kParts; ++u) {
@@ -436,8 +437,9 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         *reinterpret_cast<uint2 *>(p.out + (row0 + h) * kHeadDim + col) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
         if (p.lse != nullptr && col == 0) p.lse[row0 + h] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
       };
+      const int part_floats = paged_part_floats(p.G);
       // of a shared pair: slot 0 of a CTA whose range begins inside the pair, slot 1 of the one where the pair begins
-      float *part = p.partials + ((int64_t)blockIdx.x * 2 + (cta_first == (int)blockIdx.x ? 1 : 0)) * kPartialStride;
+      float *part = p.partials + ((int64_t)blockIdx.x * 2 + (cta_first == (int)blockIdx.x ? 1 : 0)) * part_floats;
       // the warps' results (of tiles, or of parts) as one
       auto merge_warps = [&](auto emit) {
         for (int item = tid; item < p.G * (kHeadDim / 4); item += kPaThreads) {
@@ -462,7 +464,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       } else {
         merge_warps([&](int h, int col, float4 o, float M, float l) {
           *reinterpret_cast<float4 *>(part + h * kHeadDim + col) = o;
-          if (col == 0) *reinterpret_cast<float2 *>(part + kMaxGroup * kHeadDim + 2 * h) = make_float2(M, l);
+          if (col == 0) *reinterpret_cast<float2 *>(part + p.G * kHeadDim + 2 * h) = make_float2(M, l);
         });
         SAGEKV_STAMP(6);
         const int parts = cta_last - cta_first + 1;
@@ -473,7 +475,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         SAGEKV_STAMP(7);
         if (sh.arrived == parts - 1) {                       // every other part is in scratch
           if (tid == 0) p.tickets[(int64_t)at.seq * p.H_kv + at.head] = 0;
-          const float *first = p.partials + ((int64_t)cta_first * 2 + 1) * kPartialStride;
+          const float *first = p.partials + ((int64_t)cta_first * 2 + 1) * part_floats;
           if (p.G <= 4) join_parts<4, 4>(first, parts, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
           else join_parts<2, 8>(first, parts, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
           __syncthreads();
