@@ -4,19 +4,26 @@
 // K and V of KV head h / G.  The rows are read once, so the floor is HBM: sum of the lengths * H_kv * 2 rows.
 //
 // Split.  The lengths are known on the device only (a captured launch serves later lengths), and a batch may be one
-// long sequence or many uneven ones.  So the 16-token tiles of all (sequence, KV head) pairs form one list, cut into
-// equal ranges, one per CTA; every CTA finds its range from the lengths by a block-wide scan.  A range may
-// hold the end of one pair, several whole pairs and the start of another.  Whole pairs are finished where they
-// are; of a pair that several CTAs share each leaves (maximum, sum, 128 columns) per head in scratch, and the one
-// that arrives last (a ticket per pair, no waiting) joins the parts in the order of the tokens: the result does not
-// depend on which arrives last.
+// long sequence or many uneven ones.  So all (sequence, KV head) pairs form one list of units of six 16-token tiles, a
+// tile per warp, cut into equal ranges, one per CTA; every CTA finds its range from the lengths by a scan.  A range may
+// hold the end of one pair, several whole pairs and the start of another; in front of each pair the list has two empty places, so that a
+// CTA whose range changes pairs gets that much less to do (without them those CTAs were the last ones, 10 us behind the
+// others at 131072 tokens x 8 heads).  Whole pairs are finished where they are; of a pair that several CTAs share each leaves
+// (maximum, sum, 128 columns) per head in scratch, and the one that arrives last (a ticket per pair, no waiting) joins
+// the parts, each warp always the same ones: the result does not depend on which arrives last.
 //
-// In a CTA the tiles are dealt to four warps in turn, and each works for itself: its tiles come through a private ring
-// (K and V of a tile, tensor copies counted on an mbarrier of the stage), it keeps a running maximum, the
-// sums and the whole 128-column result in registers and refills a stage as soon as it has read it.  The page id of
-// the next tile is loaded while the present one is worked on.  Products as in the streamed decode over the reduced
-// cache: S = K Q^T with tokens as rows (M = 16) and the heads as columns (N = 8), O^T += V^T P.  An 8-bit cache is
+// In a CTA each warp works for itself: its tiles come through a private ring (K and V of a tile, tensor copies counted on an
+// mbarrier of the stage), it keeps a running maximum, the sums and the whole 128-column result in registers and refills a
+// stage as soon as it has read it.  Page ids are looked up 32 tiles at a time.  Products as in the streamed decode over the
+// reduced cache: S = K Q^T with tokens as rows (M = 16) and the heads as columns (N = 8), O^T += V^T P.  An 8-bit cache is
 // staged as it is and widened to f16 (exact) between shared memory and the tensor cores.
+//
+// What bounds it.  Long caches: HBM.  Twelve warps per SM with 8 KB on the way each are enough; more bytes in flight only let some
+// SMs have more of the bandwidth than others, and the launch waits for the others (us, 8 heads x 131072 tokens / x 8
+// sequences of 32768 / 8-bit; floors 81.8 / 163.5 / 40.9, 81.8): eight warps with 24 KB each 94.6 / 171 / 59.4, 101; with 16 KB
+// 89.9 / 170 / 55.5, 99.6; twelve with 8 KB 82.8 / 161 / 46.5, 86; sixteen (128 registers) 93.6 / 168 / 53.6, 94.2.  Short ones: a chain of waits
+// (us in a launch on 8 heads x 300 tokens, 5.9 in all): the previous launch's end seen 1.1, lengths 0.6, page ids and copies issued
+// 0.9, rows there 0.4, a tile and the warps' merge 1.1, ticket 0.9, join 1.2.  Between them both (8 heads x 8192 tokens: 12.2, floor 5.1).
 //
 // A tile's rows behind the sequence's end hold anything: their scores are replaced, not added to, and their V rows are
 // cleared in the fragments, since zero times NaN is NaN.
@@ -38,7 +45,7 @@ struct PaShared {
   float o[kPaWarps][kMaxGroup * kPaHeadStride];         // results of the warps
   float2 ml[kPaWarps][kMaxGroup];                       // (max, sum) of a warp's tiles
   unsigned long long bar[kPaWarps][kPaMaxStages];
-  int start[2];                                         // where my range begins (many sequences): sequence, tiles of the list before it
+  int start[2];                                         // where my range begins (many sequences): sequence, where its places begin
   int arrived;                                          // parts of a shared pair that had arrived before mine
 };
 static_assert(kPagedCtasPerSm * (sizeof(PaShared) + 1024) <= 228 * 1024, "they fit on an SM together");
@@ -85,8 +92,9 @@ __device__ __forceinline__ int places_of(int len) { return len > 0 ? (len + 16 *
 
 // Joins the parts warp, warp + kPaWarps, ... of a shared pair (the first in slot 1 of its CTA, the others in slot 0 of theirs), kParts of
 // up to kHeads heads at a time with all their loads in flight; the result goes where a warp's result of tiles does.
-// (us from the last ticket to the end, 8 / 29 / 37 parts of four heads: a thread per four columns of a head going through
-// sixteen parts at a time 1.7 / 3.1 / 3.7, this 1.3 / 1.5 / 1.6)
+// (us from the last ticket to the end, 4 / 10 / 22 / 32 / 37 parts of four heads: 1.2 / 1.4 / 1.7 / 2.5 / 2.2.  A thread per four columns of
+// a head going through sixteen parts at a time: 1.2 at 2 parts, 1.7 at 8, 3.1 at 29, 3.7 at 37.  Six parts at a time instead of four
+// cost registers and with them the loop over the tiles: 8-bit, 8 x 32768 tokens 86.6 -> 90.2)
 template <int kParts, int kHeads>
 __device__ __forceinline__ void join_parts(const float *first, int parts, int G, int warp, int lane, float *o_to, float2 *ml_to) {
   static_assert(kParts * kHeads <= 32 && (kHeads & (kHeads - 1)) == 0, "a lane per part and head");
@@ -169,7 +177,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
   wait_for_predecessor();
   SAGEKV_STAMP(1);
 
-  // ---- my range of the list: [lo, lo + n), which begins in sequence start_seq, start_before tiles from the list's begin ----
+  // ---- my range of the list: [lo, lo + n), which begins in sequence start_seq, whose places begin at start_before ----
   const int most_tokens = p.c.max_pages * p.c.page_size;
   const uint32_t n_ctas = gridDim.x;
   uint32_t total, per_cta, lo;
@@ -194,7 +202,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       if (lane >= o) incl += v;
     }
     total = (uint32_t)__shfl_sync(0xffffffffu, incl, 31);
-    // A second CTA per pair costs a ticket and the join, 2.4 us, and saves half of the steps of 1 us (8 heads x 100 tokens 4.9 / 5.9 us
+    // A second CTA per pair costs a ticket and the join, 2.1 us, and saves half of the steps of 1 us (8 heads x 100 tokens 4.9 / 5.9 us
     // whole / cut, x 300 tokens 6.9 / 5.9).
     constexpr uint32_t kWhole = kPaPairCost + kPaWholeUnits;
     n = cut(total <= kWhole * (uint32_t)__popc(__ballot_sync(0xffffffffu, mine > 0)) ? kWhole : 1u);
@@ -368,7 +376,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
             for (int j = 0; j < 8; ++j) ldmatrix_x4_trans(tb + v_off[j], va[j][0], va[j][1], va[j][2], va[j][3]);
           }
           // ---- softmax weights ----
-          const int left = at.len - (tile << 4);    // tokens of the sequence from this tile's first on
+          const int left = at.len - (tile << 4);             // tokens of the sequence from this tile's first on
           if (left < 16) {
             if (g >= left) sv[0] = sv[1] = -INFINITY;
             if (g + 8 >= left) sv[2] = sv[3] = -INFINITY;
@@ -412,7 +420,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       }
 
       SAGEKV_STAMP_AFTER(5, acc[0][0] + acc[7][3]);
-      // ---- the pair (or my part of it) is done: merge the four warps ----
+      // ---- the pair (or my part of it) is done: merge the warps ----
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
         l0 += __shfl_xor_sync(0xffffffffu, l0, o);

@@ -177,6 +177,12 @@ enum { kTurnOnly = 0, kTurnAppend = 1, kTurnAppendE4m3 = 2 };
 
 // A warp takes rows of one kind (queries, keys or values; all of a token's, or some groups of four of them: blockIdx.y says which) of
 // one token after another.  The rows are on their way while position and page are looked up.
+// Bound by HBM where there are many tokens of bf16 (65536 x 8 KV heads 85.3 us, floor 81.8; 20011 x 28 heads rotated alone 46.3 of 43.7),
+// close to the issue rate into an 8-bit cache (73 us of 61.4: conversions and the angles against half the bytes), by latency where
+// there are few (one token 2 us).  What it took (us, 65536 tokens x 8 KV heads, bf16 / 8-bit): a warp for all rows of a token
+// 122.7 / 124.7 (1080 instructions a token); loads and angles shared out leaner, a kind per warp 100.7 / 98.6; frequencies
+// through shared memory 90.3 / 84.1; sines from the quadrant, packed instructions 88.3 / 80.4; from token to token in 72 registers
+// 85.3 / 73.0 (in 64, with spills: 90.4 / 83.4).  Rows through a ring of asynchronous copies instead: 106 / 119.
 template <int kMode>
 __global__ void __launch_bounds__(kTurnWarps * 32, kTurnCtasPerSm)
 turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp, const int q_parts, const int kv_parts) {
