@@ -314,8 +314,9 @@ cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm,
 // each lane finds one row's place (list, then table: two loads one behind the other, for all rows at once), then the
 // rows are moved kRows at a time, 16 bytes per lane, all loads ahead of the stores.  An 8-bit row is widened: code * scale,
 // rounded to bf16.  Bound by that chain of loads where the rows are few, by their scatter where they are many.  (us, 8 heads x 2049 bf16
-// rows / 16 x 8193 bf16 / 16 x 8193 8-bit: eight rows at once in blocks of eight warps, loads past L1 5.25 / 35.9 / 24.9, four in blocks
-// of four 4.1 / 25.1 / 25.6, plain loads besides 3.5 / 24.0 / 25.5; eight at once and 32 per warp 3.7 / 25.2 / 23.3)
+// rows / 16 x 8193 bf16 / 16 x 8193 8-bit; floors 2.6 / 20.5 / 15.4: eight rows at once in blocks of eight warps, loads past L1
+// 5.25 / 35.9 / 24.9, four in blocks of four 4.1 / 25.1 / 25.6, plain loads besides 3.5 / 24.0 / 25.5; 8-bit eight at once and 32 per
+// warp 23.3, with stores of whole sectors 20.4, 16 per warp 19.1; bf16 now 3.4 / 23.7)
 constexpr int kCompactWarps = 4;
 
 template <bool kE4m3, int kRows>
@@ -357,6 +358,7 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
     bool there[kLoads];
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
+      row[u] = make_uint4(0u, 0u, 0u, 0u);
       const int i = i0 + u * kAtOnce + sub;
       const int64_t at = __shfl_sync(0xffffffffu, src, i & 31);
       there[u] = i < n && at >= 0 && SAGEKV_OK_INDEX(p.c.status, first + i < L && b < p.B);
@@ -364,7 +366,6 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
     }
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      if (!there[u]) continue;
       uint16_t *o = dst + (int64_t)(i0 + u * kAtOnce + sub) * p.cs.token_stride;
       if (kE4m3) {
         const uint32_t w[4] = {row[u].x, row[u].y, row[u].z, row[u].w};
@@ -375,9 +376,18 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
           y[2 * i] = pack_bf16x2(x0.x * scale, x0.y * scale);
           y[2 * i + 1] = pack_bf16x2(x1.x * scale, x1.y * scale);
         }
-        st_v4(o, make_uint4(y[0], y[1], y[2], y[3]));
-        st_v4(o + 8, make_uint4(y[4], y[5], y[6], y[7]));
-      } else {
+        // two neighbours swap halves, so that each store writes whole sectors: first the even lane's 32 bytes, then the odd lane's
+        const bool odd = lane & 1;
+        uint4 mine = odd ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
+        uint4 other = odd ? make_uint4(y[0], y[1], y[2], y[3]) : make_uint4(y[4], y[5], y[6], y[7]);
+        other.x = __shfl_xor_sync(0xffffffffu, other.x, 1);
+        other.y = __shfl_xor_sync(0xffffffffu, other.y, 1);
+        other.z = __shfl_xor_sync(0xffffffffu, other.z, 1);
+        other.w = __shfl_xor_sync(0xffffffffu, other.w, 1);
+        if (!there[u]) continue;                               // (the same for both)
+        st_v4(odd ? o - 8 : o, odd ? other : mine);
+        st_v4(odd ? o + 8 : o + 16, odd ? mine : other);
+      } else if (there[u]) {
         st_v4(o, row[u]);
       }
     }
@@ -386,10 +396,10 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
 
 cudaError_t launch_paged_compact(const PagedCompactParams &p, int dtype, int n_sm, cudaStream_t stream) {
   const int64_t L = p.S + (int64_t)p.G * p.k_q + p.R + 1, heads = (int64_t)p.B * p.H_kv;
-  // as many rows per warp as leave every SM two dozen warps
+  // four rows per warp, of a long 8-bit launch up to sixteen, as long as that leaves every SM two dozen warps
   const bool e4m3 = dtype == SAGEKV_CACHE_E4M3;
   int rows = 4;
-  while (rows < (e4m3 ? 32 : 8) && L * heads / (2 * rows) >= (int64_t)n_sm * 24) rows *= 2;
+  while (e4m3 && rows < 16 && L * heads / (2 * rows) >= (int64_t)n_sm * 24) rows *= 2;
   const int64_t per_block = (int64_t)kCompactWarps * rows;
   const auto kernel = !e4m3 ? paged_compact_kernel<false, 4> : rows >= 8 ? paged_compact_kernel<true, 8> : paged_compact_kernel<true, 4>;
   return launch_next(kernel, dim3((unsigned)((L + per_block - 1) / per_block), (unsigned)heads), kCompactWarps * 32, 0, stream, 0, p, rows);
