@@ -400,7 +400,7 @@ int sagekv_score_static(const sagekv_shape *shape, const void *q_last, const voi
  * layout; sequences may share pages.
  *   dtype      SAGEKV_CACHE_BF16, or SAGEKV_CACHE_E4M3: 8-bit elements that stand
  *              for code * scale, one fp32 scale per KV head in k_scale / v_scale
- *              (device, [H_kv]; NULL: 1).  Scales must be positive and finite.
+ *              (device, [H_kv]; NULL: 1), each within 2^-100 .. 2^100.
  *              NULL for a bf16 cache.
  *   page_size  tokens per page, a multiple of 16.
  *   strides    in elements, multiples of 16 bytes, each at least 128 elements.
@@ -408,8 +408,8 @@ int sagekv_score_static(const sagekv_shape *shape, const void *q_last, const voi
  *   seq_lens   int32 [n_seqs], tokens in each sequence (0 is allowed); read by
  *              sagekv_paged_attn alone, may be NULL for the other calls.
  * block_table and seq_lens are device memory, read by the kernels: a captured
- * launch sees what they hold when it is replayed.  The host cannot check them, so the
- * kernels do, in every build: a page id outside [0, n_pages), a sequence or a
+ * launch sees what they hold when it is replayed.  The host cannot check them, so
+ * the kernels do, in every build: a page id outside [0, n_pages), a sequence or a
  * position outside the table, a length beyond max_pages * page_size sets bit 1
  * of the status word (sagekv_status: SAGEKV_ERR_BOUNDS) and the access is left
  * out, as each call says.  Errors of every call that takes one (see
@@ -519,15 +519,15 @@ int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sa
  *              tokens' queries, rotated beside in the same launch; q_out may
  *              be q (with the same strides).
  * Into a bf16 cache the (rotated) rows are rounded once; into an 8-bit cache the
- * fp32 values divided by the scale are rounded once to the nearest e4m3
- * value, those beyond +-448 (infinities too) to +-448, NaN to NaN.  seq_lens is neither read nor
- * changed.  No two tokens of a call may have the same sequence and position, or
- * reach the same row through shared pages: which of them a part of the row
- * would come from is undefined.  A token whose sequence, position or page id is out of range is not
- * stored (its query is rotated) and sets the status bit.
- * Errors: those of the cache, INVALID (null, exactly one of q and q_out,
- * strides below 128, negative n_tokens, a plan that no call filled), ALIGN, UNSUPPORTED (n_tokens
- * above 2^31 - 1), DEVICE, CUDA. */
+ * fp32 values divided by the scale are rounded once to the nearest e4m3 value,
+ * those beyond +-448 (infinities too) to +-448, NaN to NaN.  seq_lens is neither
+ * read nor changed.  No two tokens of a call may have the same sequence and
+ * position, or reach the same row through shared pages: which of them a part of
+ * the row would come from is undefined.  A token whose sequence, position or page
+ * id is out of range is not stored (its query is rotated) and sets the status bit.
+ * Errors: those of the cache, INVALID (null, exactly one of q and q_out, strides
+ * below 128, negative n_tokens, a plan that no call filled), ALIGN, UNSUPPORTED
+ * (n_tokens above 2^31 - 1), DEVICE, CUDA. */
 int sagekv_paged_append(sagekv_ctx *ctx, const sagekv_paged_cache *cache, const void *k, const void *v,
                         sagekv_rows kvs, int64_t n_tokens, const int32_t *positions, const int32_t *seqs,
                         const sagekv_rope_plan *plan, const void *q, sagekv_rows qs, void *q_out, sagekv_rows qos,
@@ -541,27 +541,29 @@ int sagekv_paged_append(sagekv_ctx *ctx, const sagekv_paged_cache *cache, const 
  *        of 8, at least H_q*128), heads contiguous.
  *   out  bf16 [n_seqs, H_q, 128] contiguous;  lse  fp32 [n_seqs, H_q] or NULL
  *        (natural log of the softmax denominator, maximum included).
- * A sequence without tokens gives zeros and lse = -infinity.  What a page holds behind
- * a sequence's last token is not looked at (NaN there does no harm).  A negative length counts as 0 and one beyond the
- * table as the table's; tokens whose page id is out of range are left out; both set the
- * status bit.  Rows of out and lse behind n_seqs are not touched.  The work is split
- * over the tokens by the lengths found on the device and joined by log-sum-exp
- * inside the same launch, in the order of the tokens: the same inputs give the
- * same bits.  Products and sums are fp32; the softmax weights are rounded to
- * bf16 (8-bit cache: to f16) before they multiply V.  The context's scratch is
- * used, as by the other calls: calls on one context must be ordered, captured graphs that
- * hold them too.
- * Errors: those of the cache, INVALID (null, seq_lens NULL, q_stride too small), ALIGN,
- * DEVICE, CUDA. */
+ * A sequence without tokens gives zeros and lse = -infinity.  What a page holds
+ * behind a sequence's last token is not looked at (NaN there does no harm).  A
+ * negative length counts as 0 and one beyond the table as the table's; tokens
+ * whose page id is out of range are left out; both set the status bit.  Rows of out
+ * and lse behind n_seqs are not touched.  The work is split over the tokens by the
+ * lengths found on the device and joined by log-sum-exp inside the same launch, in
+ * an order that the lengths and the table's size decide: the same inputs give the
+ * same bits on the same device.  Products and sums are fp32; the softmax weights are rounded to bf16
+ * (8-bit cache: to f16) before they multiply V.  The context's scratch is used, as
+ * by the other calls: calls on one context must be ordered, and so must replays of
+ * captured graphs that hold them.
+ * Errors: those of the cache, INVALID (null, seq_lens NULL, q_stride too small),
+ * ALIGN, DEVICE, CUDA. */
 int sagekv_paged_attn(sagekv_ctx *ctx, const void *q, int64_t q_stride, const sagekv_paged_cache *cache, void *out,
                       float *lse, void *stream);
 
 /* sagekv_score on a paged cache: every sequence has n_ctx tokens, and n_seqs
  * must be the context's batch.  Same output (the sums of a product in another
- * order), hints and errors as sagekv_score, plus those of the cache (INVALID also for n_seqs != batch or n_ctx above
- * max_pages * page_size).  From an 8-bit cache the scores are those of the values it
- * stands for.  Tokens whose page id is out of range get the score 0 and set the
- * status bit. */
+ * order), hints and errors as sagekv_score, plus those of the cache (INVALID also
+ * for n_seqs != batch or n_ctx above max_pages * page_size).  From an 8-bit cache
+ * the scores are those of the values it stands for.  Tokens whose page id is out of
+ * range get the score 0 (where no token of the region has a page, all get the same)
+ * and set the status bit. */
 int sagekv_paged_score(sagekv_ctx *ctx, const void *q_last, const sagekv_paged_cache *cache, int64_t n_ctx,
                        int32_t n_init, int32_t n_recent, float *scores, int64_t scores_row_stride, void *stream);
 
@@ -569,15 +571,15 @@ int sagekv_paged_score(sagekv_ctx *ctx, const void *q_last, const sagekv_paged_c
  * from lists that sagekv_select_topk has written.
  *   idx     int32 [batch, H_q, k_q] contiguous, k_q = min(k/G, E): offsets into
  *           the eviction region (0 is token n_init), as sagekv_select_topk leaves
- *           them for the rows of sagekv_paged_score.  The lists are taken as they are: order and
- *           repetitions are kept.  May be NULL if k_q is 0.
+ *           them for the rows of sagekv_paged_score.  The lists are taken as they
+ *           are: order and repetitions are kept.  May be NULL if k_q is 0.
  *   Kc, Vc, cs, state   as for sagekv_select_compact; rows of a bf16 cache are
  *           bit-exact copies, those of an 8-bit cache code * scale rounded to bf16.
  * Row r of a list entry or page id out of range is left as it was and sets the
  * status bit.  Every sequence has n_ctx tokens, n_seqs must be the batch.
  * Errors: those of the cache, INVALID (null, bad partition, k < 0, k % G != 0,
- * n_seqs != batch, n_ctx above max_pages * page_size), ALIGN, UNSUPPORTED (n_ctx above max_ctx, L above
- * max_len, group mode 1), DEVICE, CUDA. */
+ * n_seqs != batch, n_ctx above max_pages * page_size), ALIGN, UNSUPPORTED (n_ctx
+ * above max_ctx, L above max_len, group mode 1), DEVICE, CUDA. */
 int sagekv_paged_compact(sagekv_ctx *ctx, const int32_t *idx, const sagekv_paged_cache *cache, int64_t n_ctx,
                          int32_t n_init, int32_t n_recent, int32_t k, void *Kc, void *Vc, sagekv_strides cs,
                          sagekv_cache_state *state, void *stream);

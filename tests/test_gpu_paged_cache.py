@@ -468,6 +468,12 @@ def test_score_and_compact_with_bad_pages_and_positions(dtype):
     gone[0, 48:64] = gone[0, 192:] = gone[1, :16] = True
     assert torch.equal(p == 0, gone[:, None, S: S + E].expand(2, 2, E))
     assert torch.allclose(p.double().sum(-1), torch.ones(2, 2, device="cuda").double(), atol=1e-5)
+    pool.table[1] = -1                                              # no page at all: the row stays finite, for a selection that may follow
+    none = sk.paged_score(q, cache, N, S, R)[2:, :E]
+    assert torch.allclose(none, torch.full_like(none, 1 / E), rtol=1e-5)
+    with pytest.raises(B.SagekvError):
+        sk.status()
+    pool.table[1], pool.table[1, 0] = good[1], 2 ** 31 - 1
     idx = torch.tensor([[[0, 44, 45, 50, 90, 91], [1, 2, 3, -1, E, 2 ** 31 - 1]]] * 2, dtype=torch.int32, device="cuda")
     layer = sk.new_layer(S, R, 2 * k_q)
     layer.Kc.fill_(7.0), layer.Vc.fill_(7.0)
