@@ -397,7 +397,8 @@ int sagekv_score_static(const sagekv_shape *shape, const void *q_last, const voi
  * t / page_size], slot t % page_size, at element
  *     p*page_stride + g*head_stride + (t % page_size)*token_stride
  * of k_pages and of v_pages, 128 contiguous elements.  Both pools have the same
- * layout; sequences may share pages.
+ * layout and hold the H_kv heads of the context's shape, which the structure does
+ * not repeat; sequences may share pages.
  *   dtype      SAGEKV_CACHE_BF16, or SAGEKV_CACHE_E4M3: 8-bit elements that stand
  *              for code * scale, one fp32 scale per KV head in k_scale / v_scale
  *              (device, [H_kv]; NULL: 1), each within 2^-100 .. 2^100.

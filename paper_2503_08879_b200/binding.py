@@ -97,6 +97,7 @@ class PagedCache(C.Structure):
             if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (k_pages.shape[1],) or not s.is_contiguous()):
                 raise ValueError("expected contiguous float32 scales, one per KV head")
         self.tensors = (k_pages, v_pages, block_table, seq_lens, k_scale, v_scale)
+        self.n_kv_heads = k_pages.shape[1]
         if any(t is not None and t.device != k_pages.device for t in self.tensors):
             raise ValueError("expected all tensors of a cache on one device")
         ptr = lambda t: None if t is None else t.data_ptr()
@@ -515,8 +516,8 @@ class SageKV:
         seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
         shape = k.shape
         n, heads, _ = shape
-        if heads != self.shape[1] or v.shape != shape:
-            raise ValueError("expected k and v [tokens, H_kv, 128]")
+        if heads != self.shape[1] or v.shape != shape or cache.n_kv_heads != heads:
+            raise ValueError("expected k and v [tokens, H_kv, 128] and pages of H_kv heads")
         if not _int32_row(positions, n) or not (seqs is None or _int32_row(seqs, n)):
             raise ValueError("expected contiguous int32 positions and seqs, one per token")
         if q is not None:
@@ -533,8 +534,8 @@ class SageKV:
     def paged_attn(self, q, cache: PagedCache, out=None, lse=None):
         """Attention of one new token per sequence, q [>= n_seqs, H_q, 128], over its cache."""
         shape, n = q.shape, cache.n_seqs
-        if shape[0] < n or shape[1] != self.shape[0]:
-            raise ValueError("expected q [n_seqs, H_q, 128]")
+        if shape[0] < n or shape[1] != self.shape[0] or cache.n_kv_heads != self.shape[1]:
+            raise ValueError("expected q [n_seqs, H_q, 128] and pages of H_kv heads")
         if out is None:
             out = torch.empty(shape, dtype=q.dtype, device=q.device)
         elif out.numel() < n * shape[1] * 128 or not out.is_contiguous():
@@ -546,9 +547,9 @@ class SageKV:
 
     def paged_score(self, q_last, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, scores=None):
         """score() on a paged cache whose sequences have n_ctx tokens each."""
-        Hq, _, d, batch = self.shape
-        if q_last.numel() != batch * Hq * d or not q_last.is_contiguous():
-            raise ValueError("expected contiguous q_last [B, H_q, 128]")
+        Hq, Hkv, d, batch = self.shape
+        if q_last.numel() != batch * Hq * d or not q_last.is_contiguous() or cache.n_kv_heads != Hkv:
+            raise ValueError("expected contiguous q_last [B, H_q, 128] and pages of H_kv heads")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
         sagekv_paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
@@ -557,6 +558,8 @@ class SageKV:
     def paged_compact(self, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, layer: Layer = None):
         """The reduced cache from lists of offsets into the eviction region, int32 [B, H_q, k_q], as sagekv_select_topk writes
         them (layer.idx is not touched)."""
+        if cache.n_kv_heads != self.shape[1]:
+            raise ValueError("expected pages of H_kv heads")
         k_q = max(0, min(k // self.G, n_ctx - 1 - n_init - n_recent))
         if idx is not None and not _int32_row(idx, self.shape[3] * self.shape[0] * k_q):
             raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)]")

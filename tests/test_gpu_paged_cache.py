@@ -331,6 +331,19 @@ def test_append_out_of_range_is_left_out_and_reported(dtype):
     sk.close()
 
 
+def test_a_cache_of_another_number_of_heads_is_refused():
+    """The C structure cannot say how many heads its pages have; the binding knows, and compares."""
+    B, sk = context(4, 2, 2, max_ctx=40, max_len=40)
+    pool = O.Pool(1, 16, 2, 2, BF16, "cuda")
+    cache, k, q, pos = pool.cache(B, [5, 5]), random(2, 2, 128), random(2, 4, 128), torch.zeros(2, dtype=torch.int32, device="cuda")
+    idx = torch.zeros(2, 4, 3, dtype=torch.int32, device="cuda")
+    for call in (lambda: sk.paged_append(cache, k, k, pos), lambda: sk.paged_attn(q, cache), lambda: sk.paged_score(q, cache, 32, 4, 5),
+                 lambda: sk.paged_compact(idx, cache, 32, 4, 5, 6)):
+        with pytest.raises(ValueError):
+            call()
+    sk.close()
+
+
 def test_append_refusals():
     B, sk = context(4, 2, 3)
     pool = O.Pool(2, 16, 3, 2, BF16, "cuda")
