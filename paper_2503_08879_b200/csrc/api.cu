@@ -82,10 +82,11 @@ int sagekv_create(sagekv_ctx **out, const sagekv_shape *shape, int64_t max_ctx, 
   cudaError_t e = cudaMalloc(&ctx->score_partials, n_rows * ctx->max_chunks * sizeof(float2));
   // (the attention over pages has its scratch behind the decode step's)
   const size_t decode_floats = n_heads * ctx->max_splits * kPartialStride;
+  const size_t n_tickets = 2 * n_heads + 3 + 2 * (size_t)paged_attn_max_ctas(ctx->dev->n_sm);
   const size_t paged_floats = (size_t)paged_attn_max_ctas(ctx->dev->n_sm) * 2 * paged_part_floats(ctx->G);
   if (e == cudaSuccess) e = cudaMalloc(&ctx->decode_partials, (decode_floats + paged_floats) * sizeof(float));
-  if (e == cudaSuccess) e = cudaMalloc(&ctx->tickets, (2 * n_heads + 3) * sizeof(int32_t));
-  if (e == cudaSuccess) e = cudaMemset(ctx->tickets, 0, (2 * n_heads + 3) * sizeof(int32_t));
+  if (e == cudaSuccess) e = cudaMalloc(&ctx->tickets, n_tickets * sizeof(int32_t));
+  if (e == cudaSuccess) e = cudaMemset(ctx->tickets, 0, n_tickets * sizeof(int32_t));
   if (e == cudaSuccess) {
     ctx->status = ctx->tickets + n_heads + 1;
     ctx->paged_tickets = ctx->tickets + n_heads + 3;

@@ -17,7 +17,7 @@ struct sagekv_ctx {
   float *decode_partials;   // [B*H_kv, max_splits (clusters per head), kPartialStride]
   int max_splits;
   float *paged_partials;    // [grid of the paged attention][2][paged_part_floats(G)]: what a CTA leaves of heads that it shares (behind decode_partials)
-  int32_t *paged_tickets;   // [B*H_kv] arrival counters of the paged attention, zero between launches (behind tickets)
+  int32_t *paged_tickets;   // [B*H_kv] + [grid of the paged attention][2] arrival counters of its pairs and groups, zero between launches (behind tickets)
   int32_t *tickets;         // [B*H_kv + 1], zero between launches; the status word and the selection's ready word follow them
   int32_t *status;          // one int32: kStatus* bits raised by the kernels
   int last_cuda_error;

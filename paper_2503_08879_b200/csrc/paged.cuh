@@ -49,6 +49,7 @@ struct PagedAttnParams {
   float *lse;              // [n_seqs, H_q] or null
   float *partials;         // [CTAs][2][paged_part_floats(G)]
   int32_t *tickets;        // [n_seqs * H_kv], zero between launches
+  int32_t *group_tickets;  // [CTAs][2], zero between launches
   int G, H_q, H_kv;
   float scale_log2;
 };

@@ -222,6 +222,7 @@ int sagekv_paged_attn(sagekv_ctx *ctx, const void *q, int64_t q_stride, const sa
   p.lse = lse;
   p.partials = ctx->paged_partials;
   p.tickets = ctx->paged_tickets;
+  p.group_tickets = ctx->paged_tickets + (int64_t)ctx->shape.batch * ctx->shape.n_kv_heads;
   p.G = ctx->G;
   p.H_q = ctx->shape.n_q_heads;
   p.H_kv = ctx->shape.n_kv_heads;

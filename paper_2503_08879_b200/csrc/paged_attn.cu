@@ -38,6 +38,7 @@ constexpr int kPaRingBytes = 2 * kSlotBytes;        // per warp: one stage of bf
 constexpr int kPaHeadStride = kHeadDim + 4;         // floats between the heads of a warp's result: the 32 lanes of a store fall into 32 banks
 constexpr int kPaPairCost = 2;                      // places of the list in front of a pair's units: what a change of pair costs a CTA, in units
 constexpr int kPaWholeUnits = 2;                    // pairs that are this short in the mean are not cut where there are CTAs to spare
+constexpr int kPaRounds = 3;                        // a pair's parts are joined in groups beyond so many rounds of one CTA's warps
 constexpr int kPaMaxStages = 2;
 
 struct PaShared {
@@ -90,13 +91,14 @@ struct PaCursor {
 // places in the list that the pairs of a sequence take, per head
 __device__ __forceinline__ int places_of(int len) { return len > 0 ? (len + 16 * kPaWarps - 1) / (16 * kPaWarps) + kPaPairCost : 0; }
 
-// Joins the parts warp, warp + kPaWarps, ... of a shared pair (the first in slot 1 of its CTA, the others in slot 0 of theirs), kParts of
-// up to kHeads heads at a time with all their loads in flight; the result goes where a warp's result of tiles does.
+// Joins `count` results of a shared pair, those of its parts base, base + step, ...: each warp takes every kPaWarps-th, kParts of up to
+// kHeads heads at a time with all their loads in flight; what it has goes where a warp's result of tiles does.  (Part 0 lies in
+// slot 1 of its CTA, the others in slot 0 of theirs; part_0: slot 0 of part 0's CTA.)
 // (us from the last ticket to the end, 4 / 10 / 22 / 32 / 37 parts of four heads: 1.2 / 1.4 / 1.7 / 2.5 / 2.2.  A thread per four columns of
 // a head going through sixteen parts at a time: 1.2 at 2 parts, 1.7 at 8, 3.1 at 29, 3.7 at 37.  Six parts at a time instead of four
 // cost registers and with them the loop over the tiles: 8-bit, 8 x 32768 tokens 86.6 -> 90.2)
 template <int kParts, int kHeads>
-__device__ __forceinline__ void join_parts(const float *first, int parts, int G, int warp, int lane, float *o_to, float2 *ml_to) {
+__device__ __forceinline__ void join_parts(const float *part_0, int base, int step, int count, int G, int warp, int lane, float *o_to, float2 *ml_to) {
   static_assert(kParts * kHeads <= 32 && (kHeads & (kHeads - 1)) == 0, "a lane per part and head");
   const int u_mine = lane / kHeads, h_mine = lane & (kHeads - 1);   // the lane of part u and head h works out its weight
   float M = -INFINITY, l = 0.f;                              // of head h_mine
@@ -104,11 +106,14 @@ __device__ __forceinline__ void join_parts(const float *first, int parts, int G,
 #pragma unroll
   for (int h = 0; h < kHeads; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
   const int part_floats = paged_part_floats(G);
-  auto part_of = [&](int i) { return i == 0 ? first : first + ((int64_t)i * 2 - 1) * part_floats; };
-  for (int i0 = warp; i0 < parts; i0 += kPaWarps * kParts) {
+  auto part_of = [&](int k) {
+    const int i = base + k * step;
+    return part_0 + (int64_t)(2 * i + (i == 0 ? 1 : 0)) * part_floats;
+  };
+  for (int i0 = warp; i0 < count; i0 += kPaWarps * kParts) {
     float2 ml = make_float2(-INFINITY, 0.f);
     const int i_mine = i0 + u_mine * kPaWarps;
-    if (u_mine < kParts && i_mine < parts && h_mine < G)
+    if (u_mine < kParts && i_mine < count && h_mine < G)
       ml = __ldcg(reinterpret_cast<const float2 *>(part_of(i_mine) + G * kHeadDim + 2 * h_mine));
     float4 v[kParts][kHeads];
 #pragma unroll
@@ -117,7 +122,7 @@ __device__ __forceinline__ void join_parts(const float *first, int parts, int G,
 #pragma unroll
       for (int h = 0; h < kHeads; ++h) {
         v[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i0 + u * kPaWarps < parts && h < G) v[u][h] = __ldcg(reinterpret_cast<const float4 *>(from + h * kHeadDim));
+        if (i0 + u * kPaWarps < count && h < G) v[u][h] = __ldcg(reinterpret_cast<const float4 *>(from + h * kHeadDim));
       }
     }
     float top = fmaxf(M, ml.x);
@@ -446,8 +451,6 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         if (p.lse != nullptr && col == 0) p.lse[row0 + h] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
       };
       const int part_floats = paged_part_floats(p.G);
-      // of a shared pair: slot 0 of a CTA whose range begins inside the pair, slot 1 of the one where the pair begins
-      float *part = p.partials + ((int64_t)blockIdx.x * 2 + (cta_first == (int)blockIdx.x ? 1 : 0)) * part_floats;
       // the warps' results (of tiles, or of parts) as one
       auto merge_warps = [&](auto emit) {
         for (int item = tid; item < p.G * (kHeadDim / 4); item += kPaThreads) {
@@ -470,24 +473,45 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       if (whole) {
         merge_warps(finish);
       } else {
-        merge_warps([&](int h, int col, float4 o, float M, float l) {
-          *reinterpret_cast<float4 *>(part + h * kHeadDim + col) = o;
-          if (col == 0) *reinterpret_cast<float2 *>(part + p.G * kHeadDim + 2 * h) = make_float2(M, l);
-        });
+        auto leave = [&](float *part) {
+          merge_warps([&](int h, int col, float4 o, float M, float l) {
+            *reinterpret_cast<float4 *>(part + h * kHeadDim + col) = o;
+            if (col == 0) *reinterpret_cast<float2 *>(part + p.G * kHeadDim + 2 * h) = make_float2(M, l);
+          });
+        };
+        // slot 0 of a CTA whose range begins inside the pair, slot 1 of the one where the pair begins
+        leave(p.partials + ((int64_t)blockIdx.x * 2 + (cta_first == (int)blockIdx.x ? 1 : 0)) * part_floats);
         SAGEKV_STAMP(6);
-        const int parts = cta_last - cta_first + 1;
-        __syncthreads();
-        if (tid == 0)                                        // (behind the barrier its release stands for the whole block, and so does its acquire)
-          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(sh.arrived) : "l"(p.tickets + (int64_t)at.seq * p.H_kv + at.head) : "memory");
-        __syncthreads();
-        SAGEKV_STAMP(7);
-        if (sh.arrived == parts - 1) {                       // every other part is in scratch
-          if (tid == 0) p.tickets[(int64_t)at.seq * p.H_kv + at.head] = 0;
-          const float *first = p.partials + ((int64_t)cta_first * 2 + 1) * part_floats;
-          if (p.G <= 4) join_parts<4, 4>(first, parts, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
-          else join_parts<2, 8>(first, parts, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+        // The last CTA of the pair joins its parts; of very many (few pairs on the whole device) the last of each group of
+        // neighbours first joins the group, its result taking the place of the group's first part (one head of eight queries x
+        // 131072 tokens 34.1 -> 18.2 us, two x 32768 19.7 -> 14.5).
+        const int parts = cta_last - cta_first + 1, group_size = (p.G <= 4 ? 4 : 2) * kPaWarps;
+        float *const part_0 = p.partials + (int64_t)cta_first * 2 * part_floats;
+        bool grouped = parts > kPaRounds * group_size;
+        const int group = ((int)blockIdx.x - cta_first) / group_size;
+        int base = grouped ? group * group_size : 0, step = 1, count = grouped ? min(group_size, parts - base) : parts;
+        int32_t *const pair_ticket = p.tickets + (int64_t)at.seq * p.H_kv + at.head;
+        int32_t *ticket = grouped ? p.group_tickets + 2 * (cta_first + base) + (base == 0 ? 1 : 0) : pair_ticket;
+        for (;;) {
           __syncthreads();
-          merge_warps(finish);
+          if (tid == 0)                                      // (behind the barrier its release stands for the whole block, and so does its acquire)
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(sh.arrived) : "l"(ticket) : "memory");
+          __syncthreads();
+          SAGEKV_STAMP(7);
+          if (sh.arrived != count - 1) break;                // else every other part is in scratch
+          if (tid == 0) *ticket = 0;
+          // (beside an 8-bit cache fewer at a time: the loop over the tiles needs the registers, 8 x 32768 tokens 88.7 -> 86.1 us)
+          if (p.G <= 4) join_parts<kE4m3 ? 3 : 4, 4>(part_0, base, step, count, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+          else join_parts<kE4m3 ? 1 : 2, 8>(part_0, base, step, count, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+          __syncthreads();
+          if (!grouped) {
+            merge_warps(finish);
+            break;
+          }
+          leave(part_0 + (int64_t)(2 * base + (base == 0 ? 1 : 0)) * part_floats);
+          grouped = false;
+          base = 0; step = group_size; count = (parts + group_size - 1) / group_size;
+          ticket = pair_ticket;
         }
       }
       SAGEKV_STAMP(8);

@@ -86,6 +86,14 @@ def test_a_long_sequence_of_one_head_is_shared_by_every_cta(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("Hq, Hkv, lens", [(8, 1, [60000]), (7, 1, [9000]), (3, 1, [30000, 2, 25000]), (16, 2, [20000]), (5, 1, [40000, 40000, 1]), (1, 1, [28416]),
+                                           (8, 1, [3500, 0, 3600])])
+def test_pairs_of_very_many_parts(Hq, Hkv, lens, dtype):
+    """Up to a part per CTA: more than 36 (eight heads) or 72 (four) are joined in groups first."""
+    run(Hq, Hkv, lens, dtype=dtype, page=48)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
 def test_long_tables_and_a_batch_that_is_not_full(dtype):
     run(8, 2, [50, 2000], dtype=dtype, batch=9, max_pages=4000)
 
