@@ -519,6 +519,10 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
     }
     if (timed_out) atomicOr(p.c.status, kStatusWaitTimeout);
   }
+#if defined(SAGEKV_TRACE)
+  for (int i = 4; i < 9; ++i)                                // (a CTA without tiles, or with whole pairs alone, has not been everywhere)
+    if (trace_t[i] < trace_t[i - 1]) trace_t[i] = trace_t[i - 1];
+#endif
   SAGEKV_STAMP(9);
   SAGEKV_TRACE_END(p.q);
 }

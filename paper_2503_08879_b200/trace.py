@@ -1,11 +1,12 @@
-"""Timeline of the decode-attention (or select+compact) launches: where the time of a launch goes, CTA by CTA.
+"""Timeline of the decode-attention (select+compact, paged attention) launches: where the time of a launch goes, CTA by CTA.
 
 Builds the library with -DSAGEKV_TRACE (thread 0 of every CTA of the kernel notes the global timer at ten points;
 the normal build has none of that), replays a CUDA graph of decode calls (select calls in hint mode 2 with
-`--select`) over the layers of a workload, and prints the phases of a launch as medians over CTAs and launches.
+`--select`, of calls over a paged full cache with `--paged`) over the layers of a workload, and prints the phases of a launch as medians over CTAs and launches.
 The stamps cost a few per cent, so the microseconds per launch printed here are a little above the benchmark's.
 
     python -m paper_2503_08879_b200.trace [workload] [overlap mode] [layers] [decode variant] [--select]
+    python -m paper_2503_08879_b200.trace [workload] [tokens] [layers] --paged
 """
 
 from __future__ import annotations
@@ -26,6 +27,10 @@ NAMES = ["CTA starts", "copies issued", "dependency wait over", "K landed", "max
 # the streamed kernel (many heads, long caches); a CTA with several whole heads shows its last one
 STREAM_NAMES = ["CTA starts", "copies issued", "dependency wait over", "first tile landed", "last tile done", "results in shared memory",
                 "results sent", "inbox full", "outputs written", "CTA ends"]
+
+# (of a CTA with several pairs its last one; a phase that a CTA does not have takes no time)
+PAGED_NAMES = ["CTA starts", "dependency wait over", "range known", "copies requested", "first tile landed", "last tile done",
+               "part in scratch", "ticket taken", "pair done", "CTA ends"]
 
 
 def report(buf_reader, names, run, label, heads=1):
@@ -115,6 +120,46 @@ def trace_select(argv):
     sk.close()
 
 
+def trace_paged(argv):
+    """Attention over the whole cache in pages of 16 tokens, bf16, pages in random order."""
+    import torch
+    from . import binding as B, synth
+    name = argv[0] if len(argv) > 0 else "C3-2048"
+    w = synth.workload(name)
+    tokens = int(argv[1]) if len(argv) > 1 else w.n_ctx
+    n_layers = int(argv[2]) if len(argv) > 2 else 4
+    dev = torch.device("cuda:0")
+    sk = B.SageKV(w.n_q_heads, w.n_kv_heads, w.head_dim, w.batch, max_ctx=1024, max_len=64, device=dev)
+    width = -(-tokens // 16)
+    layers = []
+    for _ in range(n_layers):
+        k = torch.randn(w.batch * width, w.n_kv_heads, 16, w.head_dim, device=dev, dtype=torch.bfloat16)
+        table = torch.randperm(w.batch * width, device=dev).view(w.batch, width).to(torch.int32)
+        cache = B.PagedCache(k, torch.randn_like(k), table, torch.full((w.batch,), tokens, dtype=torch.int32, device=dev))
+        q = torch.randn(w.batch, w.n_q_heads, w.head_dim, device=dev, dtype=torch.bfloat16)
+        layers.append((q, cache, torch.empty_like(q)))
+    rounds = 4
+
+    def phase():
+        for _ in range(rounds):
+            for q, cache, out in layers:
+                sk.paged_attn(q, cache, out)
+
+    phase(); torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        phase()
+    for _ in range(3):
+        g.replay()
+
+    def run():
+        g.replay()
+        return rounds * n_layers
+
+    report(B.lib.sagekv_trace_read_paged, PAGED_NAMES, run, "%s shape, %d tokens in pages, %d layers" % (name, tokens, n_layers))
+    sk.close()
+
+
 def main(argv):
     from . import build
     os.environ["SAGEKV_LIB"] = build.build(trace=True)
@@ -122,6 +167,8 @@ def main(argv):
     from . import binding as B, synth
     if "--select" in argv:
         return trace_select([a for a in argv if a != "--select"])
+    if "--paged" in argv:
+        return trace_paged([a for a in argv if a != "--paged"])
     name = argv[0] if len(argv) > 0 else "C3-2048"
     overlap = int(argv[1]) if len(argv) > 1 else 2
     w = synth.workload(name)
