@@ -418,8 +418,10 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
             if (kE4m3) mma_f16_16816(acc[j][0], acc[j][1], acc[j][2], acc[j][3], va[j][0], va[j][1], va[j][2], va[j][3], b0, b1);
             else mma_bf16_16816(acc[j][0], acc[j][1], acc[j][2], acc[j][3], va[j][0], va[j][1], va[j][2], va[j][3], b0, b1);
           }
-          __syncwarp();                                      // every lane has its fragments: the stage may be refilled
         }
+        // Every lane has its fragments, and has seen this phase of the barrier: the stage may be refilled.  (Where the next tile's page is
+        // none, lane 0 completes the next phase at once: a lane that still polled for this one would then never see it.)
+        __syncwarp();
         request(stage);
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }

@@ -114,8 +114,10 @@ paged_score_kernel(const ScoreParams p, const PagedView c, const __grid_constant
       sv[0] = sv[1] = sv[2] = sv[3] = -1.0e30f;
     } else {
       score_tile<kE4m3>(ring + (uint32_t)(stage * kTileBytes), k_off, qb, mult0, mult1, sv);
-      __syncwarp();                                            // every lane has its fragments: the stage may be refilled
     }
+    // Every lane has its fragments, and has seen this phase of the barrier: the stage may be refilled.  (Where the next tile's page is
+    // none, lane 0 completes the next phase at once: a lane that still polled for this one would then never see it.)
+    __syncwarp();
     request(stage);
     if (++stage == kStages) { stage = 0; phase ^= 1u; }
     const int i0 = (tile_of(unit) << 4) + g - p.S, i1 = i0 + 8;   // places in the eviction region: the first and last tiles reach beyond
