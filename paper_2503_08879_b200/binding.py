@@ -557,7 +557,7 @@ class SageKV:
 
     def paged_compact(self, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, layer: Layer = None):
         """The reduced cache from lists of offsets into the eviction region, int32 [B, H_q, k_q], as sagekv_select_topk writes
-        them (layer.idx is not touched)."""
+        them (layer.idx is not touched).  A layer that the caller brings has to hold the rows."""
         if cache.n_kv_heads != self.shape[1]:
             raise ValueError("expected pages of H_kv heads")
         k_q = max(0, min(k // self.G, n_ctx - 1 - n_init - n_recent))
@@ -565,5 +565,11 @@ class SageKV:
             raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)]")
         if layer is None:
             layer = self.new_layer(n_init, n_recent, k)
+        else:                                          # the library is given Kc's strides for both, and no number of rows
+            Kc, Vc, (_, Hkv, d, batch) = layer.Kc, layer.Vc, self.shape
+            rows = n_init + self.G * k_q + n_recent + 1
+            if Kc.dim() != 4 or Kc.shape[2] < rows or (Kc.shape[0], Kc.shape[1], Kc.shape[3]) != (batch, Hkv, d) or Vc.shape != Kc.shape or \
+                    Vc.stride() != Kc.stride():
+                raise ValueError("expected a layer whose Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128], laid out alike")
         sagekv_paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)
         return layer

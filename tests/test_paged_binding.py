@@ -1,0 +1,86 @@
+"""What the wrapper's paged methods refuse by themselves, before the library is called (needs no device: the context is none,
+so a call that is let through comes back from the library as INVALID)."""
+
+import ctypes as C
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+HQ, HKV, BATCH = 8, 2, 3
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2503_08879_b200 import build
+    build.build()
+    from paper_2503_08879_b200 import binding as B
+    names = ("score", "select_compact", "decode_attn", "pool_scores", "quest_bounds", "select_topk")
+    bind = lambda stream: B._marshal.bind(*(C.cast(getattr(B.lib, "sagekv_" + n), C.c_void_p).value for n in names), stream, C.ArgumentError)
+    bind(lambda: 0)                                                  # there is no current stream without a device
+    yield B
+    bind(B._stream_handle)
+
+
+def wrapper(B, device_index=-1):
+    """A SageKV without a context; -1 is the index that host tensors give."""
+    sk = B.SageKV.__new__(B.SageKV)
+    sk.ctx, sk.shape, sk.G, sk.device, sk.device_index = None, (HQ, HKV, 128, BATCH), HQ // HKV, torch.device("cpu"), device_index
+    return sk
+
+
+def cache(B, lens=True, **kw):
+    k = torch.zeros(12, HKV, 16, 128, dtype=BF16)
+    return B.PagedCache(k, torch.zeros_like(k), torch.zeros(BATCH, 4, dtype=torch.int32), torch.zeros(BATCH, dtype=torch.int32) if lens else None, **kw)
+
+
+def reaches_the_library(B, call, *a, **kw):
+    with pytest.raises(B.SagekvError) as e:
+        call(*a, **kw)
+    assert e.value.code == B.ERR_INVALID
+
+
+def refused(call, *a, **kw):
+    with pytest.raises(ValueError):
+        call(*a, **kw)
+
+
+# ---- paged_compact: the caller's layer -------------------------------------------------------------------------------------
+
+N, S, R, KQ = 60, 4, 10, 5
+L = S + HQ // HKV * KQ + R + 1
+
+
+def layer_of(B, Kc, Vc):
+    return SimpleNamespace(Kc=Kc, Vc=Vc, state=B.CacheState(0, 0, 0, 0, 0, 0, None))
+
+
+def compact(B, layer, sk=None):
+    idx = torch.zeros(BATCH, HQ, KQ, dtype=torch.int32)
+    return (sk or wrapper(B)).paged_compact, idx, cache(B), N, S, R, HQ // HKV * KQ, layer
+
+
+def test_layers_that_hold_the_rows_are_taken(B):
+    for rows in (L, L + 7):
+        Kc = torch.zeros(BATCH, HKV, rows, 128, dtype=BF16)
+        reaches_the_library(B, *compact(B, layer_of(B, Kc, torch.zeros_like(Kc))))
+    wide = torch.zeros(BATCH, HKV, L, 136, dtype=BF16)
+    reaches_the_library(B, *compact(B, layer_of(B, wide[..., :128], wide.clone()[..., :128])))
+    reaches_the_library(B, *compact(B, None))
+
+
+@pytest.mark.parametrize("shape", [(BATCH, HKV, L - 1, 128), (BATCH - 1, HKV, L, 128), (BATCH, HKV - 1, L, 128), (BATCH, HKV, L, 64),
+                                   (BATCH, HKV, L * 128), (HKV, L, 128)])
+def test_layers_too_small_for_the_rows_are_refused(B, shape):
+    """A layer of a smaller budget, or of another batch: the rows would go into the next head's, and past the end."""
+    small, full = torch.zeros(shape, dtype=BF16), torch.zeros(BATCH, HKV, L, 128, dtype=BF16)
+    for Kc, Vc in ((small, small.clone()), (full, small), (small, full)):
+        refused(*compact(B, layer_of(B, Kc, Vc)))
+
+
+def test_a_layer_whose_tensors_are_laid_out_differently_is_refused(B):
+    """One set of strides goes to the library, Kc's."""
+    Kc = torch.zeros(BATCH, HKV, L, 128, dtype=BF16)
+    refused(*compact(B, layer_of(B, Kc, torch.zeros(BATCH, L, HKV, 128, dtype=BF16).transpose(1, 2))))
+    refused(*compact(B, layer_of(B, torch.zeros(BATCH, HKV, L + 1, 128, dtype=BF16), Kc)))
