@@ -505,7 +505,9 @@ class SageKV:
             out = torch.empty(shape, dtype=x.dtype, device=x.device)
         elif out.shape != shape:
             raise ValueError("expected out with the shape of x")
-        n, heads, _ = shape
+        n, heads, d = shape
+        if d != 128:
+            raise ValueError("expected rows [tokens, heads, 128]")
         if not _int32_row(positions, n):
             raise ValueError("expected contiguous int32 positions, one per token")
         sagekv_rope(self.ctx, plan, x, n, heads, positions, out)
@@ -515,8 +517,8 @@ class SageKV:
         """Keys and values [tokens, H_kv, 128] into their pages, keys (and queries q, into q_out) rotated by the plan.  Without
         seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
         shape = k.shape
-        n, heads, _ = shape
-        if heads != self.shape[1] or v.shape != shape or cache.n_kv_heads != heads:
+        n, heads, d = shape
+        if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads:
             raise ValueError("expected k and v [tokens, H_kv, 128] and pages of H_kv heads")
         if not _int32_row(positions, n) or not (seqs is None or _int32_row(seqs, n)):
             raise ValueError("expected contiguous int32 positions and seqs, one per token")
@@ -526,7 +528,7 @@ class SageKV:
                 q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
             elif q_out is not q and q_out.shape != shape:
                 raise ValueError("expected q_out with the shape of q")
-            if shape[0] != n or shape[1] != self.shape[0]:
+            if shape != (n, self.shape[0], 128):
                 raise ValueError("expected q [tokens, H_q, 128]")
         sagekv_paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
         return q_out
@@ -534,7 +536,7 @@ class SageKV:
     def paged_attn(self, q, cache: PagedCache, out=None, lse=None):
         """Attention of one new token per sequence, q [>= n_seqs, H_q, 128], over its cache."""
         shape, n = q.shape, cache.n_seqs
-        if shape[0] < n or shape[1] != self.shape[0] or cache.n_kv_heads != self.shape[1]:
+        if len(shape) != 3 or shape[0] < n or shape[1] != self.shape[0] or shape[2] != 128 or cache.n_kv_heads != self.shape[1]:
             raise ValueError("expected q [n_seqs, H_q, 128] and pages of H_kv heads")
         if out is None:
             out = torch.empty(shape, dtype=q.dtype, device=q.device)

@@ -84,3 +84,40 @@ def test_a_layer_whose_tensors_are_laid_out_differently_is_refused(B):
     Kc = torch.zeros(BATCH, HKV, L, 128, dtype=BF16)
     refused(*compact(B, layer_of(B, Kc, torch.zeros(BATCH, L, HKV, 128, dtype=BF16).transpose(1, 2))))
     refused(*compact(B, layer_of(B, torch.zeros(BATCH, HKV, L + 1, 128, dtype=BF16), Kc)))
+
+
+# ---- rows of 128 -----------------------------------------------------------------------------------------------------------
+
+
+def rows(*shape, dtype=BF16):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+def int32(n):
+    return torch.zeros(n, dtype=torch.int32)
+
+
+def test_calls_with_whole_rows_reach_the_library(B):
+    sk, c, plan = wrapper(B), cache(B), B.sagekv_rope_plan(128, False, 1e4)
+    reaches_the_library(B, sk.rope, rows(5, 3, 128), int32(5), plan)
+    reaches_the_library(B, sk.rope, rows(5, 3, 136)[..., 8:], int32(5), plan, rows(5, 4, 128)[:, :3])
+    reaches_the_library(B, sk.paged_append, c, rows(5, HKV, 128), rows(5, HKV, 128), int32(5), int32(5), plan, rows(5, HQ, 128))
+    reaches_the_library(B, sk.paged_append, c, rows(5, HKV, 128), rows(5, HKV, 128), int32(5))
+    reaches_the_library(B, sk.paged_attn, rows(BATCH, HQ, 128), c)
+    reaches_the_library(B, sk.paged_attn, rows(BATCH + 2, HQ, 128), c, rows(BATCH, HQ, 128), torch.zeros(BATCH, HQ))
+    reaches_the_library(B, sk.paged_score, rows(BATCH, HQ, 128), c, N, S, R, torch.zeros(BATCH * HQ, 60))
+
+
+def test_rows_that_are_shorter_are_refused(B):
+    """128 elements are read and written per row: half a row of a wider tensor has the strides of a whole one, and the result that the
+    wrapper would make for it is too short."""
+    sk, c, plan = wrapper(B), cache(B), B.sagekv_rope_plan(64, False, 1e4)
+    half = lambda *shape: rows(*shape)[..., :64]
+    refused(sk.paged_attn, half(BATCH, HQ, 128), c)
+    refused(sk.paged_attn, rows(BATCH, HQ, 64), c)
+    refused(sk.rope, rows(1, 1, 64), int32(1), plan)
+    refused(sk.rope, half(5, 3, 128), int32(5), plan)
+    k, q = rows(1, HKV, 128), rows(1, HQ, 128)
+    refused(sk.paged_append, c, half(1, HKV, 128), half(1, HKV, 128), int32(1))
+    refused(sk.paged_append, c, k, k, int32(1), None, plan, half(1, HQ, 128))
+    refused(sk.paged_append, c, k, k, int32(1), None, plan, q, half(1, HQ, 128))
