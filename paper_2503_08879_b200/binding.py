@@ -397,7 +397,8 @@ def sagekv_decode_attn(ctx, q, k_new, v_new, Kc, Vc, state: CacheState, out, lse
         _check(code, "sagekv_decode_attn", ctx)
 
 
-_INT32 = torch.int32
+_INT32, _BF16, _FP32 = torch.int32, torch.bfloat16, torch.float32
+_typed = _marshal.typed
 
 
 def _int32_row(t, n: int) -> bool:
@@ -506,8 +507,8 @@ class SageKV:
         elif out.shape != shape:
             raise ValueError("expected out with the shape of x")
         n, heads, d = shape
-        if d != 128:
-            raise ValueError("expected rows [tokens, heads, 128]")
+        if d != 128 or not _typed(_BF16, x, out):
+            raise ValueError("expected bf16 rows [tokens, heads, 128]")
         if not _int32_row(positions, n):
             raise ValueError("expected contiguous int32 positions, one per token")
         sagekv_rope(self.ctx, plan, x, n, heads, positions, out)
@@ -518,8 +519,8 @@ class SageKV:
         seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
         shape = k.shape
         n, heads, d = shape
-        if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads:
-            raise ValueError("expected k and v [tokens, H_kv, 128] and pages of H_kv heads")
+        if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads or not _typed(_BF16, k, v):
+            raise ValueError("expected bf16 k and v [tokens, H_kv, 128] and pages of H_kv heads")
         if not _int32_row(positions, n) or not (seqs is None or _int32_row(seqs, n)):
             raise ValueError("expected contiguous int32 positions and seqs, one per token")
         if q is not None:
@@ -528,8 +529,8 @@ class SageKV:
                 q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
             elif q_out is not q and q_out.shape != shape:
                 raise ValueError("expected q_out with the shape of q")
-            if shape != (n, self.shape[0], 128):
-                raise ValueError("expected q [tokens, H_q, 128]")
+            if shape != (n, self.shape[0], 128) or not _typed(_BF16, q, q_out):
+                raise ValueError("expected bf16 q and q_out [tokens, H_q, 128]")
         sagekv_paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
         return q_out
 
@@ -544,6 +545,8 @@ class SageKV:
             raise ValueError("expected contiguous out [n_seqs, H_q, 128]")
         if lse is not None and (lse.numel() < n * shape[1] or not lse.is_contiguous()):
             raise ValueError("expected contiguous lse [n_seqs, H_q]")
+        if not _typed(_BF16, q, out) or not _typed(_FP32, lse):
+            raise ValueError("expected bf16 q and out, fp32 lse")
         sagekv_paged_attn(self.ctx, q, cache, out, lse)
         return out
 
@@ -554,6 +557,8 @@ class SageKV:
             raise ValueError("expected contiguous q_last [B, H_q, 128] and pages of H_kv heads")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
+        if not _typed(_BF16, q_last) or not _typed(_FP32, scores):
+            raise ValueError("expected bf16 q_last and fp32 scores")
         sagekv_paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
         return scores
 
@@ -571,7 +576,7 @@ class SageKV:
             Kc, Vc, (_, Hkv, d, batch) = layer.Kc, layer.Vc, self.shape
             rows = n_init + self.G * k_q + n_recent + 1
             if Kc.dim() != 4 or Kc.shape[2] < rows or (Kc.shape[0], Kc.shape[1], Kc.shape[3]) != (batch, Hkv, d) or Vc.shape != Kc.shape or \
-                    Vc.stride() != Kc.stride():
-                raise ValueError("expected a layer whose Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128], laid out alike")
+                    Vc.stride() != Kc.stride() or not _typed(_BF16, Kc, Vc):
+                raise ValueError("expected a layer whose bf16 Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128], laid out alike")
         sagekv_paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)
         return layer

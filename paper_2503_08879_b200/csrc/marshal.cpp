@@ -41,7 +41,7 @@ PagedScoreFn g_paged_score;
 PagedCompactFn g_paged_compact;
 PyObject *g_stream_of;   // callable: handle of the current stream of the current device, as an integer
 PyObject *g_arg_error;   // ctypes.ArgumentError
-PyObject *g_data_ptr, *g_stride;
+PyObject *g_data_ptr, *g_stride, *g_dtype;
 
 // All of these return false with a Python exception set.
 bool pointer(PyObject *t, void **out) {
@@ -103,6 +103,15 @@ bool rows(PyObject *t, sagekv_rows *out) {
     return false;
   }
   out->token_stride = s[0]; out->head_stride = s[1];
+  return true;
+}
+
+// is t of this type?  (types are single objects)
+bool of_type(PyObject *t, PyObject *dtype, bool *yes) {
+  PyObject *v = PyObject_GetAttr(t, g_dtype);
+  if (v == nullptr) return false;
+  *yes = v == dtype;
+  Py_DECREF(v);
   return true;
 }
 
@@ -305,6 +314,14 @@ PyObject *paged_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// dtype, tensors: is each (None: passed over) of that type?
+PyObject *typed(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  bool yes = n > 0;
+  for (Py_ssize_t i = 1; yes && i < n; ++i)
+    if (a[i] != Py_None && !of_type(a[i], a[0], &yes)) return nullptr;
+  return PyBool_FromLong(yes);
+}
+
 // addresses of the paged cache's entry points (rope, paged_append, paged_attn, paged_score, paged_compact)
 PyObject *bind_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!count(n, 5)) return nullptr;
@@ -348,6 +365,7 @@ PyCFunction fast(PyObject *(*f)(PyObject *, PyObject *const *, Py_ssize_t)) {
 PyMethodDef g_methods[] = {
     {"bind", fast(bind), METH_FASTCALL, nullptr},
     {"bind_paged", fast(bind_paged), METH_FASTCALL, nullptr},
+    {"typed", fast(typed), METH_FASTCALL, nullptr},
     {"rope", fast(rope), METH_FASTCALL, nullptr},
     {"paged_append", fast(paged_append), METH_FASTCALL, nullptr},
     {"paged_attn", fast(paged_attn), METH_FASTCALL, nullptr},
@@ -368,6 +386,7 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_method
 PyMODINIT_FUNC PyInit__marshal(void) {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
   g_stride = PyUnicode_InternFromString("stride");
-  if (g_data_ptr == nullptr || g_stride == nullptr) return nullptr;
+  g_dtype = PyUnicode_InternFromString("dtype");
+  if (g_data_ptr == nullptr || g_stride == nullptr || g_dtype == nullptr) return nullptr;
   return PyModule_Create(&g_module);
 }

@@ -121,3 +121,32 @@ def test_rows_that_are_shorter_are_refused(B):
     refused(sk.paged_append, c, half(1, HKV, 128), half(1, HKV, 128), int32(1))
     refused(sk.paged_append, c, k, k, int32(1), None, plan, half(1, HQ, 128))
     refused(sk.paged_append, c, k, k, int32(1), None, plan, q, half(1, HQ, 128))
+
+
+# ---- types -------------------------------------------------------------------------------------------------------------------
+
+
+def test_tensors_of_other_types_are_refused(B):
+    """Pointers carry no type: 16-bit floats of another kind would be taken for bf16, and an lse of 2-byte elements be written past its end."""
+    sk, c, plan = wrapper(B), cache(B), B.sagekv_rope_plan(128, False, 1e4)
+    for dtype in (torch.float16, torch.float32):
+        x = rows(5, 3, 128, dtype=dtype)
+        refused(sk.rope, x, int32(5), plan)
+        refused(sk.rope, x, int32(5), plan, x)
+        refused(sk.rope, rows(5, 3, 128), int32(5), plan, x)
+        k, q, other = rows(5, HKV, 128), rows(5, HQ, 128), rows(5, HKV, 128, dtype=dtype)
+        refused(sk.paged_append, c, other, other, int32(5))
+        refused(sk.paged_append, c, k, other, int32(5))
+        refused(sk.paged_append, c, other, k, int32(5))
+        refused(sk.paged_append, c, k, k, int32(5), None, plan, rows(5, HQ, 128, dtype=dtype))
+        refused(sk.paged_append, c, k, k, int32(5), None, plan, q, rows(5, HQ, 128, dtype=dtype))
+        q = rows(BATCH, HQ, 128)
+        refused(sk.paged_attn, q.to(dtype), c)
+        refused(sk.paged_attn, q, c, q.to(dtype))
+        refused(sk.paged_score, q.to(dtype), c, N, S, R, torch.zeros(BATCH * HQ, 60))
+        full = torch.zeros(BATCH, HKV, L, 128, dtype=dtype)
+        refused(*compact(B, layer_of(B, full, full.clone())))
+        refused(*compact(B, layer_of(B, full.to(BF16), full)))
+    for dtype in (BF16, torch.float16, torch.float64):
+        refused(sk.paged_attn, q, c, None, torch.zeros(BATCH, HQ, dtype=dtype))
+        refused(sk.paged_score, q, c, N, S, R, torch.zeros(BATCH * HQ, 60, dtype=dtype))
