@@ -100,6 +100,7 @@ class PagedCache(C.Structure):
         self.n_kv_heads = k_pages.shape[1]
         if any(t is not None and t.device != k_pages.device for t in self.tensors):
             raise ValueError("expected all tensors of a cache on one device")
+        self.device_index = k_pages.get_device()
         ptr = lambda t: None if t is None else t.data_ptr()
         super().__init__(ptr(k_pages), ptr(v_pages), k_pages.stride(0), k_pages.stride(1), k_pages.stride(2), ptr(block_table),
                          block_table.stride(0) if n_seqs > 1 else max_pages, ptr(seq_lens), ptr(k_scale), ptr(v_scale), k_pages.shape[0],
@@ -398,11 +399,7 @@ def sagekv_decode_attn(ctx, q, k_new, v_new, Kc, Vc, state: CacheState, out, lse
 
 
 _INT32, _BF16, _FP32 = torch.int32, torch.bfloat16, torch.float32
-_typed = _marshal.typed
-
-
-def _int32_row(t, n: int) -> bool:
-    return t.dtype is _INT32 and t.numel() == n and t.is_contiguous()
+_placed, _placed_row = _marshal.placed, _marshal.placed_row
 
 
 class Layer:
@@ -435,6 +432,7 @@ class SageKV:
         self.shape = (n_q_heads, n_kv_heads, head_dim, batch)
         self.G = n_q_heads // n_kv_heads
         with torch.cuda.device(self.device):
+            self.device_index = torch.cuda.current_device()
             self.ctx = sagekv_create(n_q_heads, n_kv_heads, head_dim, batch, max_ctx, max_len, softmax_scale)
 
     def set_overlap(self, mode: int):
@@ -507,10 +505,10 @@ class SageKV:
         elif out.shape != shape:
             raise ValueError("expected out with the shape of x")
         n, heads, d = shape
-        if d != 128 or not _typed(_BF16, x, out):
-            raise ValueError("expected bf16 rows [tokens, heads, 128]")
-        if not _int32_row(positions, n):
-            raise ValueError("expected contiguous int32 positions, one per token")
+        if d != 128 or not _placed(_BF16, self.device_index, x, out):
+            raise ValueError("expected bf16 rows [tokens, heads, 128] on the context's device")
+        if not _placed_row(_INT32, self.device_index, n, positions):
+            raise ValueError("expected contiguous int32 positions on the context's device, one per token")
         sagekv_rope(self.ctx, plan, x, n, heads, positions, out)
         return out
 
@@ -519,24 +517,26 @@ class SageKV:
         seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
         shape = k.shape
         n, heads, d = shape
-        if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads or not _typed(_BF16, k, v):
-            raise ValueError("expected bf16 k and v [tokens, H_kv, 128] and pages of H_kv heads")
-        if not _int32_row(positions, n) or not (seqs is None or _int32_row(seqs, n)):
-            raise ValueError("expected contiguous int32 positions and seqs, one per token")
+        device = self.device_index
+        if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads or cache.device_index != device or \
+                not _placed(_BF16, device, k, v):
+            raise ValueError("expected bf16 k and v [tokens, H_kv, 128] and pages of H_kv heads on the context's device")
+        if not _placed_row(_INT32, device, n, positions) or not (seqs is None or _placed_row(_INT32, device, n, seqs)):
+            raise ValueError("expected contiguous int32 positions and seqs on the context's device, one per token")
         if q is not None:
             shape = q.shape
             if q_out is None:
                 q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
             elif q_out is not q and q_out.shape != shape:
                 raise ValueError("expected q_out with the shape of q")
-            if shape != (n, self.shape[0], 128) or not _typed(_BF16, q, q_out):
-                raise ValueError("expected bf16 q and q_out [tokens, H_q, 128]")
+            if shape != (n, self.shape[0], 128) or not _placed(_BF16, device, q, q_out):
+                raise ValueError("expected bf16 q and q_out [tokens, H_q, 128] on the context's device")
         sagekv_paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
         return q_out
 
     def paged_attn(self, q, cache: PagedCache, out=None, lse=None):
         """Attention of one new token per sequence, q [>= n_seqs, H_q, 128], over its cache."""
-        shape, n = q.shape, cache.n_seqs
+        shape, n, device = q.shape, cache.n_seqs, self.device_index
         if len(shape) != 3 or shape[0] < n or shape[1] != self.shape[0] or shape[2] != 128 or cache.n_kv_heads != self.shape[1]:
             raise ValueError("expected q [n_seqs, H_q, 128] and pages of H_kv heads")
         if out is None:
@@ -545,8 +545,8 @@ class SageKV:
             raise ValueError("expected contiguous out [n_seqs, H_q, 128]")
         if lse is not None and (lse.numel() < n * shape[1] or not lse.is_contiguous()):
             raise ValueError("expected contiguous lse [n_seqs, H_q]")
-        if not _typed(_BF16, q, out) or not _typed(_FP32, lse):
-            raise ValueError("expected bf16 q and out, fp32 lse")
+        if cache.device_index != device or not _placed(_BF16, device, q, out) or not _placed(_FP32, device, lse):
+            raise ValueError("expected bf16 q and out, fp32 lse and pages on the context's device")
         sagekv_paged_attn(self.ctx, q, cache, out, lse)
         return out
 
@@ -557,26 +557,28 @@ class SageKV:
             raise ValueError("expected contiguous q_last [B, H_q, 128] and pages of H_kv heads")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
-        if not _typed(_BF16, q_last) or not _typed(_FP32, scores):
-            raise ValueError("expected bf16 q_last and fp32 scores")
+        device = self.device_index
+        if cache.device_index != device or not _placed(_BF16, device, q_last) or not _placed(_FP32, device, scores):
+            raise ValueError("expected bf16 q_last, fp32 scores and pages on the context's device")
         sagekv_paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
         return scores
 
     def paged_compact(self, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, layer: Layer = None):
         """The reduced cache from lists of offsets into the eviction region, int32 [B, H_q, k_q], as sagekv_select_topk writes
         them (layer.idx is not touched).  A layer that the caller brings has to hold the rows."""
-        if cache.n_kv_heads != self.shape[1]:
-            raise ValueError("expected pages of H_kv heads")
+        device = self.device_index
+        if cache.n_kv_heads != self.shape[1] or cache.device_index != device:
+            raise ValueError("expected pages of H_kv heads on the context's device")
         k_q = max(0, min(k // self.G, n_ctx - 1 - n_init - n_recent))
-        if idx is not None and not _int32_row(idx, self.shape[3] * self.shape[0] * k_q):
-            raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)]")
+        if idx is not None and not _placed_row(_INT32, device, self.shape[3] * self.shape[0] * k_q, idx):
+            raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)] on the context's device")
         if layer is None:
             layer = self.new_layer(n_init, n_recent, k)
         else:                                          # the library is given Kc's strides for both, and no number of rows
             Kc, Vc, (_, Hkv, d, batch) = layer.Kc, layer.Vc, self.shape
             rows = n_init + self.G * k_q + n_recent + 1
             if Kc.dim() != 4 or Kc.shape[2] < rows or (Kc.shape[0], Kc.shape[1], Kc.shape[3]) != (batch, Hkv, d) or Vc.shape != Kc.shape or \
-                    Vc.stride() != Kc.stride() or not _typed(_BF16, Kc, Vc):
-                raise ValueError("expected a layer whose bf16 Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128], laid out alike")
+                    Vc.stride() != Kc.stride() or not _placed(_BF16, device, Kc, Vc):
+                raise ValueError("expected a layer whose bf16 Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128] on the context's device, laid out alike")
         sagekv_paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)
         return layer

@@ -8,6 +8,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <initializer_list>
+
 #include "sagekv.h"
 
 namespace {
@@ -41,7 +43,7 @@ PagedScoreFn g_paged_score;
 PagedCompactFn g_paged_compact;
 PyObject *g_stream_of;   // callable: handle of the current stream of the current device, as an integer
 PyObject *g_arg_error;   // ctypes.ArgumentError
-PyObject *g_data_ptr, *g_stride, *g_dtype;
+PyObject *g_data_ptr, *g_stride, *g_dtype, *g_get_device, *g_numel, *g_is_contiguous;
 
 // All of these return false with a Python exception set.
 bool pointer(PyObject *t, void **out) {
@@ -106,12 +108,25 @@ bool rows(PyObject *t, sagekv_rows *out) {
   return true;
 }
 
-// is t of this type?  (types are single objects)
-bool of_type(PyObject *t, PyObject *dtype, bool *yes) {
+// what a method without arguments returns: an integer (or a truth value)
+bool number(PyObject *t, PyObject *method, int64_t *out) {
+  PyObject *v = PyObject_CallMethodNoArgs(t, method);
+  if (v == nullptr) return false;
+  *out = PyLong_AsLongLong(v);
+  Py_DECREF(v);
+  return PyErr_Occurred() == nullptr;
+}
+
+// is t of this type (types are single objects), on this device?
+bool of_kind(PyObject *t, PyObject *dtype, int64_t device, bool *yes) {
   PyObject *v = PyObject_GetAttr(t, g_dtype);
   if (v == nullptr) return false;
   *yes = v == dtype;
   Py_DECREF(v);
+  if (!*yes) return true;
+  int64_t on;
+  if (!number(t, g_get_device, &on)) return false;
+  *yes = on == device;
   return true;
 }
 
@@ -314,12 +329,25 @@ PyObject *paged_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// dtype, tensors: is each (None: passed over) of that type?
-PyObject *typed(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  bool yes = n > 0;
-  for (Py_ssize_t i = 1; yes && i < n; ++i)
-    if (a[i] != Py_None && !of_type(a[i], a[0], &yes)) return nullptr;
+// dtype, device, tensors: is each (None: passed over) of that type, on that device?
+PyObject *placed(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  int64_t device;
+  if (n < 2) return PyErr_Format(PyExc_TypeError, "expected a type and a device");
+  if (!integer(a[1], &device)) return nullptr;
+  bool yes = true;
+  for (Py_ssize_t i = 2; yes && i < n; ++i)
+    if (a[i] != Py_None && !of_kind(a[i], a[0], device, &yes)) return nullptr;
   return PyBool_FromLong(yes);
+}
+
+// dtype, device, n, tensor: is it of that type, on that device, and n elements one behind the other?
+PyObject *placed_row(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  int64_t device, want, elements, contiguous;
+  bool yes;
+  if (!count(n, 4) || !integer(a[1], &device) || !integer(a[2], &want) || !of_kind(a[3], a[0], device, &yes) || !number(a[3], g_numel, &elements) ||
+      !number(a[3], g_is_contiguous, &contiguous))
+    return nullptr;
+  return PyBool_FromLong(yes && elements == want && contiguous != 0);
 }
 
 // addresses of the paged cache's entry points (rope, paged_append, paged_attn, paged_score, paged_compact)
@@ -365,7 +393,8 @@ PyCFunction fast(PyObject *(*f)(PyObject *, PyObject *const *, Py_ssize_t)) {
 PyMethodDef g_methods[] = {
     {"bind", fast(bind), METH_FASTCALL, nullptr},
     {"bind_paged", fast(bind_paged), METH_FASTCALL, nullptr},
-    {"typed", fast(typed), METH_FASTCALL, nullptr},
+    {"placed", fast(placed), METH_FASTCALL, nullptr},
+    {"placed_row", fast(placed_row), METH_FASTCALL, nullptr},
     {"rope", fast(rope), METH_FASTCALL, nullptr},
     {"paged_append", fast(paged_append), METH_FASTCALL, nullptr},
     {"paged_attn", fast(paged_attn), METH_FASTCALL, nullptr},
@@ -387,6 +416,10 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
   g_stride = PyUnicode_InternFromString("stride");
   g_dtype = PyUnicode_InternFromString("dtype");
-  if (g_data_ptr == nullptr || g_stride == nullptr || g_dtype == nullptr) return nullptr;
+  g_get_device = PyUnicode_InternFromString("get_device");
+  g_numel = PyUnicode_InternFromString("numel");
+  g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  for (PyObject *name : {g_data_ptr, g_stride, g_dtype, g_get_device, g_numel, g_is_contiguous})
+    if (name == nullptr) return nullptr;
   return PyModule_Create(&g_module);
 }

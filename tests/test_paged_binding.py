@@ -150,3 +150,56 @@ def test_tensors_of_other_types_are_refused(B):
     for dtype in (BF16, torch.float16, torch.float64):
         refused(sk.paged_attn, q, c, None, torch.zeros(BATCH, HQ, dtype=dtype))
         refused(sk.paged_score, q, c, N, S, R, torch.zeros(BATCH * HQ, 60, dtype=dtype))
+
+
+# ---- devices -----------------------------------------------------------------------------------------------------------------
+
+
+def test_tensors_on_another_device_than_the_context_are_refused(B):
+    """Host pointers, or those of another device, would reach the kernels.  (A context of device 0 here, tensors of the host.)"""
+    c, plan = cache(B), B.sagekv_rope_plan(128, False, 1e4)
+    k, q = rows(5, HKV, 128), rows(BATCH, HQ, 128)
+    for call in (lambda sk: sk.rope(rows(5, 3, 128), int32(5), plan), lambda sk: sk.paged_append(c, k, k, int32(5)),
+                 lambda sk: sk.paged_attn(q, c), lambda sk: sk.paged_score(q, c, N, S, R, torch.zeros(BATCH * HQ, 60))):
+        reaches_the_library(B, call, wrapper(B))
+        refused(call, wrapper(B, 0))
+    layer = B.Layer(BATCH, HQ, HKV, 128, L, KQ, "cpu")
+    reaches_the_library(B, *compact(B, layer))
+    refused(*compact(B, layer, wrapper(B, 0)))
+
+
+class Elsewhere:
+    """A tensor that says it is on another device."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 1
+
+
+def test_every_tensor_of_a_call_is_looked_at(B):
+    sk, plan, far = wrapper(B), B.sagekv_rope_plan(128, False, 1e4), Elsewhere
+    c, k, q, pos = cache(B), rows(5, HKV, 128), rows(5, HQ, 128), int32(5)
+    moved = cache(B)
+    moved.device_index = 1                                           # as of pages on that device
+    refused(sk.rope, far(q), pos, plan, q)
+    refused(sk.rope, q, far(pos), plan)
+    refused(sk.rope, q, pos, plan, far(q))
+    for bad in ((moved, k, k, pos, pos, plan, q, q), (c, far(k), k, pos, pos, plan, q, q), (c, k, far(k), pos, pos, plan, q, q),
+                (c, k, k, far(pos), pos, plan, q, q), (c, k, k, pos, far(pos), plan, q, q), (c, k, k, pos, pos, plan, far(q), q),
+                (c, k, k, pos, pos, plan, q, far(q))):
+        refused(sk.paged_append, *bad)
+    q, out, lse, scores = rows(BATCH, HQ, 128), rows(BATCH, HQ, 128), torch.zeros(BATCH, HQ), torch.zeros(BATCH * HQ, 60)
+    for bad in ((q, moved, out, lse), (far(q), c, out, lse), (q, c, far(out), lse), (q, c, out, far(lse))):
+        refused(sk.paged_attn, *bad)
+    for bad in ((q, moved, N, S, R, scores), (far(q), c, N, S, R, scores), (q, c, N, S, R, far(scores))):
+        refused(sk.paged_score, *bad)
+    call, idx, c, *sizes, layer = compact(B, B.Layer(BATCH, HQ, HKV, 128, L, KQ, "cpu"))
+    refused(call, idx, moved, *sizes, layer)
+    refused(call, far(idx), c, *sizes, layer)
+    refused(call, idx, c, *sizes, layer_of(B, far(layer.Kc), layer.Vc))
+    refused(call, idx, c, *sizes, layer_of(B, layer.Kc, far(layer.Vc)))
