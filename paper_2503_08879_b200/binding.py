@@ -399,7 +399,12 @@ def sagekv_decode_attn(ctx, q, k_new, v_new, Kc, Vc, state: CacheState, out, lse
 
 
 _INT32, _BF16, _FP32 = torch.int32, torch.bfloat16, torch.float32
-_placed, _placed_row = _marshal.placed, _marshal.placed_row
+_placed, _placed_row, _holds_rows = _marshal.placed, _marshal.placed_row, _marshal.holds_rows
+
+
+def _holds(Kc, Vc, sk, rows: int) -> bool:
+    """Are Kc and Vc bf16 [B, H_kv, >= rows, 128] on the context's device, laid out alike?"""
+    return _holds_rows(Kc, Vc, sk.shape[3], sk.shape[1], rows) and _placed(_BF16, sk.device_index, Kc, Vc)
 
 
 class Layer:
@@ -411,6 +416,15 @@ class Layer:
         self.idx = torch.zeros(batch, n_q_heads, max(1, k_q_cap), dtype=torch.int32, device=device)
         self.step = torch.zeros(1, dtype=torch.int32, device=device)
         self.state = CacheState(0, 0, 0, 0, 0, 0, self.step.data_ptr())
+        self._made = (self.Kc, self.Vc, batch, n_kv_heads, self.Kc.get_device(), L_cap)
+
+    def holds(self, sk, rows: int) -> bool:
+        """Has it `rows` rows for every head of the context, on its device?  (Told from how it was made, as long as the tensors are those: a
+        call of few rows would spend a third of its host time on looking at them.)"""
+        Kc, Vc, batch, heads, device, room = self._made
+        if Kc is not self.Kc or Vc is not self.Vc:
+            return _holds(self.Kc, self.Vc, sk, rows)
+        return room >= rows and sk.shape[3] == batch and sk.shape[1] == heads and sk.device_index == device
 
     def indices(self) -> torch.Tensor:
         """Selected positions as [B, H_q, k_q] for the k_q the last select_compact call used."""
@@ -507,9 +521,11 @@ class SageKV:
         n, heads, d = shape
         if d != 128 or not _placed(_BF16, self.device_index, x, out):
             raise ValueError("expected bf16 rows [tokens, heads, 128] on the context's device")
-        if not _placed_row(_INT32, self.device_index, n, positions):
+        if not _placed_row(_INT32, self.device_index, n, positions, False):
             raise ValueError("expected contiguous int32 positions on the context's device, one per token")
-        sagekv_rope(self.ctx, plan, x, n, heads, positions, out)
+        code = _marshal.rope(self.ctx, plan, x, n, heads, positions, out)
+        if code:
+            _check(code, "sagekv_rope", self.ctx)
         return out
 
     def paged_append(self, cache: PagedCache, k, v, positions, seqs=None, plan: RopePlan = None, q=None, q_out=None):
@@ -521,7 +537,7 @@ class SageKV:
         if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads or cache.device_index != device or \
                 not _placed(_BF16, device, k, v):
             raise ValueError("expected bf16 k and v [tokens, H_kv, 128] and pages of H_kv heads on the context's device")
-        if not _placed_row(_INT32, device, n, positions) or not (seqs is None or _placed_row(_INT32, device, n, seqs)):
+        if not _placed_row(_INT32, device, n, positions, False) or not (seqs is None or _placed_row(_INT32, device, n, seqs, False)):
             raise ValueError("expected contiguous int32 positions and seqs on the context's device, one per token")
         if q is not None:
             shape = q.shape
@@ -531,36 +547,41 @@ class SageKV:
                 raise ValueError("expected q_out with the shape of q")
             if shape != (n, self.shape[0], 128) or not _placed(_BF16, device, q, q_out):
                 raise ValueError("expected bf16 q and q_out [tokens, H_q, 128] on the context's device")
-        sagekv_paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
+        code = _marshal.paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
+        if code:
+            _check(code, "sagekv_paged_append", self.ctx)
         return q_out
 
     def paged_attn(self, q, cache: PagedCache, out=None, lse=None):
         """Attention of one new token per sequence, q [>= n_seqs, H_q, 128], over its cache."""
         shape, n, device = q.shape, cache.n_seqs, self.device_index
-        if len(shape) != 3 or shape[0] < n or shape[1] != self.shape[0] or shape[2] != 128 or cache.n_kv_heads != self.shape[1]:
-            raise ValueError("expected q [n_seqs, H_q, 128] and pages of H_kv heads")
+        if len(shape) != 3 or shape[0] < n or shape[1] != self.shape[0] or shape[2] != 128 or not _placed(_BF16, device, q) or \
+                cache.n_kv_heads != self.shape[1] or cache.device_index != device:
+            raise ValueError("expected bf16 q [n_seqs, H_q, 128] and pages of H_kv heads on the context's device")
+        rows = n * shape[1]
         if out is None:
             out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        elif out.numel() < n * shape[1] * 128 or not out.is_contiguous():
-            raise ValueError("expected contiguous out [n_seqs, H_q, 128]")
-        if lse is not None and (lse.numel() < n * shape[1] or not lse.is_contiguous()):
-            raise ValueError("expected contiguous lse [n_seqs, H_q]")
-        if cache.device_index != device or not _placed(_BF16, device, q, out) or not _placed(_FP32, device, lse):
-            raise ValueError("expected bf16 q and out, fp32 lse and pages on the context's device")
-        sagekv_paged_attn(self.ctx, q, cache, out, lse)
+        elif not _placed_row(_BF16, device, rows * 128, out, True):
+            raise ValueError("expected contiguous bf16 out [n_seqs, H_q, 128] on the context's device")
+        if lse is not None and not _placed_row(_FP32, device, rows, lse, True):
+            raise ValueError("expected contiguous fp32 lse [n_seqs, H_q] on the context's device")
+        code = _marshal.paged_attn(self.ctx, q, cache, out, lse)
+        if code:
+            _check(code, "sagekv_paged_attn", self.ctx)
         return out
 
     def paged_score(self, q_last, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, scores=None):
         """score() on a paged cache whose sequences have n_ctx tokens each."""
-        Hq, Hkv, d, batch = self.shape
-        if q_last.numel() != batch * Hq * d or not q_last.is_contiguous() or cache.n_kv_heads != Hkv:
-            raise ValueError("expected contiguous q_last [B, H_q, 128] and pages of H_kv heads")
+        (Hq, Hkv, d, batch), device = self.shape, self.device_index
+        if not _placed_row(_BF16, device, batch * Hq * d, q_last, False) or cache.n_kv_heads != Hkv or cache.device_index != device:
+            raise ValueError("expected contiguous bf16 q_last [B, H_q, 128] and pages of H_kv heads on the context's device")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
-        device = self.device_index
-        if cache.device_index != device or not _placed(_BF16, device, q_last) or not _placed(_FP32, device, scores):
-            raise ValueError("expected bf16 q_last, fp32 scores and pages on the context's device")
-        sagekv_paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
+        elif not _placed(_FP32, device, scores):
+            raise ValueError("expected fp32 scores on the context's device")
+        code = _marshal.paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
+        if code:
+            _check(code, "sagekv_paged_score", self.ctx)
         return scores
 
     def paged_compact(self, idx, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, k: int, layer: Layer = None):
@@ -570,15 +591,17 @@ class SageKV:
         if cache.n_kv_heads != self.shape[1] or cache.device_index != device:
             raise ValueError("expected pages of H_kv heads on the context's device")
         k_q = max(0, min(k // self.G, n_ctx - 1 - n_init - n_recent))
-        if idx is not None and not _placed_row(_INT32, device, self.shape[3] * self.shape[0] * k_q, idx):
+        if idx is not None and not _placed_row(_INT32, device, self.shape[3] * self.shape[0] * k_q, idx, False):
             raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)] on the context's device")
         if layer is None:
             layer = self.new_layer(n_init, n_recent, k)
         else:                                          # the library is given Kc's strides for both, and no number of rows
-            Kc, Vc, (_, Hkv, d, batch) = layer.Kc, layer.Vc, self.shape
             rows = n_init + self.G * k_q + n_recent + 1
-            if Kc.dim() != 4 or Kc.shape[2] < rows or (Kc.shape[0], Kc.shape[1], Kc.shape[3]) != (batch, Hkv, d) or Vc.shape != Kc.shape or \
-                    Vc.stride() != Kc.stride() or not _placed(_BF16, device, Kc, Vc):
-                raise ValueError("expected a layer whose bf16 Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128] on the context's device, laid out alike")
-        sagekv_paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)
+            fits = layer.holds(self, rows) if type(layer) is Layer else _holds(layer.Kc, layer.Vc, self, rows)
+            if not fits:
+                raise ValueError("expected a layer whose bf16 Kc and Vc are [B, H_kv, >= n_init + G * k_q + n_recent + 1, 128] on the context's "
+                                 "device, laid out alike")
+        code = _marshal.paged_compact(self.ctx, idx, cache, n_ctx, n_init, n_recent, k, layer.Kc, layer.Vc, layer.state)
+        if code:
+            _check(code, "sagekv_paged_compact", self.ctx)
         return layer

@@ -43,7 +43,7 @@ PagedScoreFn g_paged_score;
 PagedCompactFn g_paged_compact;
 PyObject *g_stream_of;   // callable: handle of the current stream of the current device, as an integer
 PyObject *g_arg_error;   // ctypes.ArgumentError
-PyObject *g_data_ptr, *g_stride, *g_dtype, *g_get_device, *g_numel, *g_is_contiguous;
+PyObject *g_data_ptr, *g_stride, *g_dtype, *g_shape, *g_get_device, *g_numel, *g_is_contiguous;
 
 // All of these return false with a Python exception set.
 bool pointer(PyObject *t, void **out) {
@@ -340,14 +340,39 @@ PyObject *placed(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return PyBool_FromLong(yes);
 }
 
-// dtype, device, n, tensor: is it of that type, on that device, and n elements one behind the other?
+// dtype, device, n, tensor, more: is it of that type, on that device, and n elements (or, if `more`, at least n) one behind the other?
 PyObject *placed_row(PyObject *, PyObject *const *a, Py_ssize_t n) {
   int64_t device, want, elements, contiguous;
   bool yes;
-  if (!count(n, 4) || !integer(a[1], &device) || !integer(a[2], &want) || !of_kind(a[3], a[0], device, &yes) || !number(a[3], g_numel, &elements) ||
+  if (!count(n, 5) || !integer(a[1], &device) || !integer(a[2], &want) || !of_kind(a[3], a[0], device, &yes) || !number(a[3], g_numel, &elements) ||
       !number(a[3], g_is_contiguous, &contiguous))
     return nullptr;
-  return PyBool_FromLong(yes && elements == want && contiguous != 0);
+  return PyBool_FromLong(yes && contiguous != 0 && (elements == want || (elements > want && a[4] == Py_True)));
+}
+
+// Kc, Vc, batch, heads, rows: are both [batch, heads, at least so many rows, 128], with the same shape and strides?
+PyObject *holds_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  int64_t want[3];
+  if (!count(n, 5) || !integer(a[2], &want[0]) || !integer(a[3], &want[1]) || !integer(a[4], &want[2])) return nullptr;
+  PyObject *shape = PyObject_GetAttr(a[0], g_shape), *shape_v = shape != nullptr ? PyObject_GetAttr(a[1], g_shape) : nullptr;
+  PyObject *strides = shape_v != nullptr ? PyObject_CallMethodNoArgs(a[0], g_stride) : nullptr;
+  PyObject *strides_v = strides != nullptr ? PyObject_CallMethodNoArgs(a[1], g_stride) : nullptr;
+  int yes = -1;
+  if (strides_v != nullptr) {
+    yes = PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 4;
+    for (int i = 0; yes == 1 && i < 4; ++i) {
+      const int64_t size = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+      yes = i == 2 ? size >= want[2] : size == (i == 3 ? 128 : want[i]);
+    }
+    if (PyErr_Occurred() != nullptr) yes = -1;
+    if (yes == 1) yes = PyObject_RichCompareBool(shape, shape_v, Py_EQ);
+    if (yes == 1) yes = PyObject_RichCompareBool(strides, strides_v, Py_EQ);
+  }
+  Py_XDECREF(shape);
+  Py_XDECREF(shape_v);
+  Py_XDECREF(strides);
+  Py_XDECREF(strides_v);
+  return yes < 0 ? nullptr : PyBool_FromLong(yes);
 }
 
 // addresses of the paged cache's entry points (rope, paged_append, paged_attn, paged_score, paged_compact)
@@ -394,6 +419,7 @@ PyMethodDef g_methods[] = {
     {"bind", fast(bind), METH_FASTCALL, nullptr},
     {"bind_paged", fast(bind_paged), METH_FASTCALL, nullptr},
     {"placed", fast(placed), METH_FASTCALL, nullptr},
+    {"holds_rows", fast(holds_rows), METH_FASTCALL, nullptr},
     {"placed_row", fast(placed_row), METH_FASTCALL, nullptr},
     {"rope", fast(rope), METH_FASTCALL, nullptr},
     {"paged_append", fast(paged_append), METH_FASTCALL, nullptr},
@@ -416,10 +442,11 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
   g_stride = PyUnicode_InternFromString("stride");
   g_dtype = PyUnicode_InternFromString("dtype");
+  g_shape = PyUnicode_InternFromString("shape");
   g_get_device = PyUnicode_InternFromString("get_device");
   g_numel = PyUnicode_InternFromString("numel");
   g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  for (PyObject *name : {g_data_ptr, g_stride, g_dtype, g_get_device, g_numel, g_is_contiguous})
+  for (PyObject *name : {g_data_ptr, g_stride, g_dtype, g_shape, g_get_device, g_numel, g_is_contiguous})
     if (name == nullptr) return nullptr;
   return PyModule_Create(&g_module);
 }

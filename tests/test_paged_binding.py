@@ -203,3 +203,16 @@ def test_every_tensor_of_a_call_is_looked_at(B):
     refused(call, far(idx), c, *sizes, layer)
     refused(call, idx, c, *sizes, layer_of(B, far(layer.Kc), layer.Vc))
     refused(call, idx, c, *sizes, layer_of(B, layer.Kc, far(layer.Vc)))
+
+
+def test_layers_of_the_wrapper_are_judged_by_how_they_were_made_unless_their_tensors_were_exchanged(B):
+    made = lambda batch=BATCH, heads=HKV, rows=L: B.Layer(batch, HQ, heads, 128, rows, KQ, "cpu")
+    reaches_the_library(B, *compact(B, made()))
+    for small in (made(rows=L - 1), made(batch=BATCH - 1), made(heads=HKV - 1)):
+        refused(*compact(B, small))
+    layer = made()
+    layer.Vc = layer.Vc[:, :, : L - 1]
+    refused(*compact(B, layer))
+    layer = made(rows=L - 1)
+    layer.Kc, layer.Vc = torch.zeros(BATCH, HKV, L, 128, dtype=BF16), torch.zeros(BATCH, HKV, L, 128, dtype=BF16)
+    reaches_the_library(B, *compact(B, layer))
