@@ -577,9 +577,10 @@ class SageKV:
             raise ValueError("expected contiguous bf16 q_last [B, H_q, 128] and pages of H_kv heads on the context's device")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
-        elif not _placed(_FP32, device, scores):
-            raise ValueError("expected fp32 scores on the context's device")
-        code = _marshal.paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, scores.stride(0))
+        shape, strides = scores.shape, scores.stride()
+        if len(shape) != 2 or shape[0] < batch * Hq or shape[1] < n_ctx - 1 - n_init - n_recent or strides[1] != 1 or not _placed(_FP32, device, scores):
+            raise ValueError("expected fp32 scores [B * H_q, >= n_ctx - 1 - n_init - n_recent] with contiguous rows on the context's device")
+        code = _marshal.paged_score(self.ctx, q_last, cache, n_ctx, n_init, n_recent, scores, strides[0])
         if code:
             _check(code, "sagekv_paged_score", self.ctx)
         return scores

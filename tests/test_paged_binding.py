@@ -216,3 +216,16 @@ def test_layers_of_the_wrapper_are_judged_by_how_they_were_made_unless_their_ten
     layer = made(rows=L - 1)
     layer.Kc, layer.Vc = torch.zeros(BATCH, HKV, L, 128, dtype=BF16), torch.zeros(BATCH, HKV, L, 128, dtype=BF16)
     reaches_the_library(B, *compact(B, layer))
+
+
+# ---- the scores' rows ----------------------------------------------------------------------------------------------------------
+
+
+def test_scores_without_a_row_per_query_head_are_refused(B):
+    """The library is given the distance of the rows and no number: a buffer of fewer rows, or of shorter ones, would be written past its end."""
+    sk, c, q, E = wrapper(B), cache(B), rows(BATCH, HQ, 128), N - 1 - S - R
+    for good in (torch.zeros(BATCH * HQ, E + 3), torch.zeros(BATCH * HQ + 1, 64), torch.zeros(BATCH * HQ, 80)[:, :E]):
+        reaches_the_library(B, sk.paged_score, q, c, N, S, R, good)
+    for bad in (torch.zeros(BATCH * HQ - 1, 64), torch.zeros(HQ, 64), torch.zeros(BATCH * HQ, E - 1), torch.zeros(64, BATCH * HQ).t(),
+                torch.zeros(BATCH, HQ, 64), torch.zeros(BATCH * HQ * 64)):
+        refused(sk.paged_score, q, c, N, S, R, bad)
