@@ -529,8 +529,8 @@ class SageKV:
         return out
 
     def paged_append(self, cache: PagedCache, k, v, positions, seqs=None, plan: RopePlan = None, q=None, q_out=None):
-        """Keys and values [tokens, H_kv, 128] into their pages, keys (and queries q, into q_out) rotated by the plan.  Without
-        seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
+        """Keys and values [tokens, H_kv, 128] (with the same strides) into their pages, keys (and queries q, into q_out) rotated by the
+        plan.  Without seqs token t belongs to sequence t.  Returns the rotated queries, or None."""
         shape = k.shape
         n, heads, d = shape
         device = self.device_index

@@ -286,7 +286,7 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
       !rows(a[3], &vs) || !integer(a[4], &tokens) || !pointer(a[5], &pos) || !pointer(a[6], &seqs) || !plan.get(a[7], "RopePlan") ||
       !pointer(a[8], &q) || !rows(a[8], &qs) || !pointer(a[9], &q_out) || !rows(a[9], &qos) || !current_stream(&stream))
     return nullptr;
-  if (ks.token_stride != vs.token_stride || ks.head_stride != vs.head_stride) {
+  if ((tokens > 1 && ks.token_stride != vs.token_stride) || ks.head_stride != vs.head_stride) {
     PyErr_SetString(PyExc_ValueError, "expected k and v with the same strides");
     return nullptr;
   }

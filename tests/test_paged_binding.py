@@ -229,3 +229,16 @@ def test_scores_without_a_row_per_query_head_are_refused(B):
     for bad in (torch.zeros(BATCH * HQ - 1, 64), torch.zeros(HQ, 64), torch.zeros(BATCH * HQ, E - 1), torch.zeros(64, BATCH * HQ).t(),
                 torch.zeros(BATCH, HQ, 64), torch.zeros(BATCH * HQ * 64)):
         refused(sk.paged_score, q, c, N, S, R, bad)
+
+
+# ---- strides that are never stepped along ---------------------------------------------------------------------------------------
+
+
+def test_one_token_of_k_and_v_out_of_different_tensors(B):
+    """Of a single token the distance of the tokens means nothing: k by itself and v out of a fused projection go together."""
+    sk, c = wrapper(B), cache(B)
+    fused = rows(1, HQ + 2 * HKV, 128)
+    reaches_the_library(B, sk.paged_append, c, rows(1, HKV, 128), fused[:, HQ + HKV:], int32(1))
+    fused = rows(2, HQ + 2 * HKV, 128)
+    refused(sk.paged_append, c, rows(2, HKV, 128), fused[:, HQ + HKV:], int32(2))
+    refused(sk.paged_append, c, rows(1, HKV, 128), rows(1, HKV, 136)[..., :128], int32(1))
