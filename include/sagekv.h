@@ -503,7 +503,7 @@ int sagekv_rope_plan_from(sagekv_rope_plan *plan, int32_t rotary_dim, int32_t in
  * n_heads need not be one of the context's head counts.  n_tokens or n_heads 0
  * launches nothing.  Errors: INVALID (null, negative sizes, strides below 128 where
  * there is more than one token or head, a plan that no call filled), ALIGN,
- * UNSUPPORTED (n_tokens above 2^31 - 1), DEVICE, CUDA. */
+ * UNSUPPORTED (n_tokens above 2^31 - 1, n_heads above 2097120), DEVICE, CUDA. */
 int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sagekv_rows xs, int64_t n_tokens,
                 int32_t n_heads, const int32_t *positions, void *out, sagekv_rows os, void *stream);
 

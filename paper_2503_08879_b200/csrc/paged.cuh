@@ -72,6 +72,8 @@ struct PagedAppendParams {
   int64_t n_tokens;
   int H_q, H_kv;
 };
+constexpr int kTurnMostQuads = 8;                                  // groups of four rows of a token that a warp takes at most
+constexpr int kRopeMostHeads = 65535 * kTurnMostQuads * 4;         // what a grid's second dimension covers
 cudaError_t launch_rope(const PagedAppendParams &p, int n_sm, cudaStream_t stream);   // the queries alone (H_q of them; every position counts)
 cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm, cudaStream_t stream);
 

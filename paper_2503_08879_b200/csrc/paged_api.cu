@@ -148,7 +148,7 @@ int sagekv_rope_plan_init(sagekv_rope_plan *plan, int32_t rotary_dim, int32_t in
 int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sagekv_rows xs, int64_t n_tokens, int32_t n_heads,
                 const int32_t *positions, void *out, sagekv_rows os, void *stream) {
   if (ctx == nullptr || plan == nullptr || !plan_ok(plan) || n_tokens < 0 || n_heads < 0) return SAGEKV_ERR_INVALID;
-  if (n_tokens > 0x7fffffff) return SAGEKV_ERR_UNSUPPORTED;
+  if (n_tokens > 0x7fffffff || n_heads > kRopeMostHeads) return SAGEKV_ERR_UNSUPPORTED;
   if (!on_own_device(ctx)) return SAGEKV_ERR_DEVICE;
   if (n_tokens == 0 || n_heads == 0) return SAGEKV_OK;
   if (x == nullptr || out == nullptr || positions == nullptr || !rows_apart(xs, n_tokens, n_heads) || !rows_apart(os, n_tokens, n_heads))

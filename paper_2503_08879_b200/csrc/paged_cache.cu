@@ -291,9 +291,9 @@ static cudaError_t launch_turn(const PagedAppendParams &p, int n_sm, cudaStream_
   const int q_quads = kMode == kTurnOnly || p.q != nullptr ? (p.H_q + 3) / 4 : 0, kv_quads = kMode == kTurnOnly ? 0 : (p.H_kv + 3) / 4;
   const int64_t warps = (int64_t)n_sm * kTurnWarps * kTurnCtasPerSm;   // that run at once
   const int64_t share = p.n_tokens * (q_quads + 2 * kv_quads) / warps;
-  const int per_warp = (int)(share < 1 ? 1 : share > 8 ? 8 : share);
+  const int per_warp = (int)(share < 1 ? 1 : share > kTurnMostQuads ? kTurnMostQuads : share);
+  // (at most 65535 parts: a launch of fewer than kTurnMostQuads a warp has fewer groups than that, and the API bounds the heads of the others)
   const int q_parts = (q_quads + per_warp - 1) / per_warp, kv_parts = (kv_quads + per_warp - 1) / per_warp, parts = q_parts + 2 * kv_parts;
-  if (parts > 65535) return cudaErrorInvalidValue;
   const int64_t rounds = p.n_tokens * parts / (kTurnWaves * warps);    // tokens of a warp, if kTurnWaves waves of blocks are to remain
   const int64_t tokens = (p.n_tokens + (rounds > 1 ? rounds : 1) - 1) / (rounds > 1 ? rounds : 1);
   return launch_next(turn_rows_kernel<kMode>, dim3((unsigned)((tokens + kTurnWarps - 1) / kTurnWarps), (unsigned)parts), kTurnWarps * 32, 0,
