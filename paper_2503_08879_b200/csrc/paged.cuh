@@ -36,6 +36,13 @@ __host__ __device__ inline int64_t paged_row(int page, int n_pages, int slot, in
   return (int64_t)page * page_stride + (int64_t)head * head_stride + (int64_t)slot * token_stride;
 }
 
+#if defined(__CUDACC__)
+// checked build: is this an entry of a sequence's row of the table?
+#define SAGEKV_OK_ENTRY(c, seq, entry) SAGEKV_OK_INDEX((c).status, (seq) >= 0 && (seq) < (c).n_seqs && (entry) >= 0 && (entry) < (c).max_pages)
+// checked build: do these 16 rows lie in a page, and in one of its heads?
+#define SAGEKV_OK_TILE(c, slot, head, H_kv) SAGEKV_OK_INDEX((c).status, (slot) >= 0 && (slot) + 16 <= (c).page_size && (head) >= 0 && (head) < (H_kv))
+#endif
+
 // ---- attention of one token per sequence over its pages -------------------------------------------------------
 constexpr int kPagedCtasPerSm = 2;
 constexpr int paged_attn_max_ctas(int n_sm) { return kPagedCtasPerSm * n_sm; }
@@ -51,6 +58,7 @@ struct PagedAttnParams {
   int32_t *tickets;        // [n_seqs * H_kv], zero between launches
   int32_t *group_tickets;  // [CTAs][2], zero between launches
   int G, H_q, H_kv;
+  int most_ctas, n_tickets;   // extents of the scratch (looked at in the checked build): CTAs with parts and group tickets, pair tickets
   float scale_log2;
 };
 cudaError_t launch_paged_attn(const PagedAttnParams &p, int dtype, int n_sm, cudaStream_t stream);

@@ -156,6 +156,7 @@ int sagekv_rope(sagekv_ctx *ctx, const sagekv_rope_plan *plan, const void *x, sa
   if (!aligned16(x) || !aligned16(out) || !rows_aligned(xs) || !rows_aligned(os)) return SAGEKV_ERR_ALIGN;
   PagedAppendParams p = {};
   p.rope = rope_args(plan);
+  p.c.status = ctx->status;
   p.q = static_cast<const uint16_t *>(x);
   p.q_out = static_cast<uint16_t *>(out);
   p.q_token = xs.token_stride;
@@ -226,6 +227,8 @@ int sagekv_paged_attn(sagekv_ctx *ctx, const void *q, int64_t q_stride, const sa
   p.G = ctx->G;
   p.H_q = ctx->shape.n_q_heads;
   p.H_kv = ctx->shape.n_kv_heads;
+  p.most_ctas = paged_attn_max_ctas(ctx->dev->n_sm);
+  p.n_tickets = ctx->shape.batch * ctx->shape.n_kv_heads;
   p.scale_log2 = ctx->scale * kLog2e;
   return done(ctx, launch_paged_attn(p, cache->dtype, ctx->dev->n_sm, static_cast<cudaStream_t>(stream)));
 }

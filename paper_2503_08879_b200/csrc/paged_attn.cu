@@ -98,22 +98,26 @@ __device__ __forceinline__ int places_of(int len) { return len > 0 ? (len + 16 *
 // a head going through sixteen parts at a time: 1.2 at 2 parts, 1.7 at 8, 3.1 at 29, 3.7 at 37.  Six parts at a time instead of four
 // cost registers and with them the loop over the tiles: 8-bit, 8 x 32768 tokens 86.6 -> 90.2)
 template <int kParts, int kHeads>
-__device__ __forceinline__ void join_parts(const float *part_0, int base, int step, int count, int G, int warp, int lane, float *o_to, float2 *ml_to) {
+__device__ __forceinline__ void join_parts(const PagedAttnParams &p, const float *part_0, int base, int step, int count, int warp, int lane, float *o_to,
+                                           float2 *ml_to) {
   static_assert(kParts * kHeads <= 32 && (kHeads & (kHeads - 1)) == 0, "a lane per part and head");
   const int u_mine = lane / kHeads, h_mine = lane & (kHeads - 1);   // the lane of part u and head h works out its weight
   float M = -INFINITY, l = 0.f;                              // of head h_mine
   float4 o[kHeads];
 #pragma unroll
   for (int h = 0; h < kHeads; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int part_floats = paged_part_floats(G);
+  const int G = p.G, part_floats = paged_part_floats(G);
   auto part_of = [&](int k) {
     const int i = base + k * step;
     return part_0 + (int64_t)(2 * i + (i == 0 ? 1 : 0)) * part_floats;
   };
+  auto in_scratch = [&](int k) {
+    return SAGEKV_OK_INDEX(p.c.status, part_of(k) >= p.partials && part_of(k) + part_floats <= p.partials + (int64_t)p.most_ctas * 2 * part_floats);
+  };
   for (int i0 = warp; i0 < count; i0 += kPaWarps * kParts) {
     float2 ml = make_float2(-INFINITY, 0.f);
     const int i_mine = i0 + u_mine * kPaWarps;
-    if (u_mine < kParts && i_mine < count && h_mine < G)
+    if (u_mine < kParts && i_mine < count && h_mine < G && in_scratch(i_mine))
       ml = __ldcg(reinterpret_cast<const float2 *>(part_of(i_mine) + G * kHeadDim + 2 * h_mine));
     float4 v[kParts][kHeads];
 #pragma unroll
@@ -122,7 +126,7 @@ __device__ __forceinline__ void join_parts(const float *part_0, int base, int st
 #pragma unroll
       for (int h = 0; h < kHeads; ++h) {
         v[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i0 + u * kPaWarps < count && h < G) v[u][h] = __ldcg(reinterpret_cast<const float4 *>(from + h * kHeadDim));
+        if (i0 + u * kPaWarps < count && h < G && in_scratch(i0 + u * kPaWarps)) v[u][h] = __ldcg(reinterpret_cast<const float4 *>(from + h * kHeadDim));
       }
     }
     float top = fmaxf(M, ml.x);
@@ -278,7 +282,8 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
     if (moved || next.unit - ids_unit >= 32) {
       ids_unit = next.unit;
       const int tile = (next.unit + lane) * kPaWarps + warp;
-      ids = tile < next.tiles() ? p.c.table[(int64_t)next.seq * p.c.table_stride + page_of(tile << 4, p.c.page_size, p.c.page_magic)] : -1;
+      const int entry = page_of(tile << 4, p.c.page_size, p.c.page_magic);
+      ids = tile < next.tiles() && SAGEKV_OK_ENTRY(p.c, next.seq, entry) ? p.c.table[(int64_t)next.seq * p.c.table_stride + entry] : -1;
     }
     const int first = (next.unit * kPaWarps + warp) << 4;
     next_slot = first - page_of(first, p.c.page_size, p.c.page_magic) * p.c.page_size;
@@ -287,7 +292,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
   auto request = [&](int s) {
     if (!more) return;
     const uint32_t bar = bars + 8u * s;
-    if (next_page >= 0 && next_page < p.c.n_pages) {
+    if (next_page >= 0 && next_page < p.c.n_pages && SAGEKV_OK_TILE(p.c, next_slot, next.head, p.H_kv)) {
       absent &= ~(1u << s);
       if (lane == 0) mbar_expect_tx(bar, kStageBytes);
       __syncwarp();
@@ -345,7 +350,10 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       const int tiles = at.tiles(), unit_end = min(at.units(), (int)(hi - at.base));
       uint32_t qb[8][2];
       float mult0, mult1;
-      load_queries<kE4m3>(p.q + (int64_t)at.seq * p.q_stride + at.head * p.G * kHeadDim, p.G, p.c.k_scale, at.head, p.scale_log2, lane, qb, mult0, mult1);
+      // (in the checked build a pair that is none is worked on as pair 0, and its result left out)
+      const bool a_pair = SAGEKV_OK_INDEX(p.c.status, at.seq < p.c.n_seqs && at.head < p.H_kv && at.seq * p.H_kv + at.head < p.n_tickets);
+      const int q_seq = a_pair ? at.seq : 0, q_head = a_pair ? at.head : 0;
+      load_queries<kE4m3>(p.q + (int64_t)q_seq * p.q_stride + q_head * p.G * kHeadDim, p.G, p.c.k_scale, q_head, p.scale_log2, lane, qb, mult0, mult1);
 
       float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // the maxima are kept kWeightShift below the scores'
       float acc[8][4];
@@ -445,7 +453,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
       const int cta_first = (int)(at.base / per_cta), cta_last = (int)((at.base + (uint32_t)at.units() - 1u) / per_cta);
       const bool whole = cta_first == cta_last;
       const int64_t row0 = (int64_t)at.seq * p.H_q + at.head * p.G;   // the pair's first row of out and lse
-      const float v_scale = kE4m3 && p.c.v_scale != nullptr ? p.c.v_scale[at.head] : 1.f;
+      const float v_scale = kE4m3 && p.c.v_scale != nullptr ? p.c.v_scale[q_head] : 1.f;
       auto finish = [&](int h, int col, float4 o, float M, float l) {
         if (!SAGEKV_OK_INDEX(p.c.status, at.seq < p.c.n_seqs && (at.head + 1) * p.G <= p.H_q && h < p.G)) return;
         const float inv = l == 0.f ? 0.f : v_scale / l;
@@ -476,6 +484,7 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         merge_warps(finish);
       } else {
         auto leave = [&](float *part) {
+          if (!SAGEKV_OK_INDEX(p.c.status, part >= p.partials && part + part_floats <= p.partials + (int64_t)p.most_ctas * 2 * part_floats)) return;
           merge_warps([&](int h, int col, float4 o, float M, float l) {
             *reinterpret_cast<float4 *>(part + h * kHeadDim + col) = o;
             if (col == 0) *reinterpret_cast<float2 *>(part + p.G * kHeadDim + 2 * h) = make_float2(M, l);
@@ -496,6 +505,9 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
         int32_t *ticket = grouped ? p.group_tickets + 2 * (cta_first + base) + (base == 0 ? 1 : 0) : pair_ticket;
         for (;;) {
           __syncthreads();
+          if (!SAGEKV_OK_INDEX(p.c.status, (ticket >= p.tickets && ticket < p.tickets + p.n_tickets) ||
+                                               (ticket >= p.group_tickets && ticket < p.group_tickets + 2 * p.most_ctas)))
+            break;
           if (tid == 0)                                      // (behind the barrier its release stands for the whole block, and so does its acquire)
             asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(sh.arrived) : "l"(ticket) : "memory");
           __syncthreads();
@@ -503,8 +515,8 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
           if (sh.arrived != count - 1) break;                // else every other part is in scratch
           if (tid == 0) *ticket = 0;
           // (beside an 8-bit cache fewer at a time: the loop over the tiles needs the registers, 8 x 32768 tokens 88.7 -> 86.1 us)
-          if (p.G <= 4) join_parts<kE4m3 ? 3 : 4, 4>(part_0, base, step, count, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
-          else join_parts<kE4m3 ? 1 : 2, 8>(part_0, base, step, count, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+          if (p.G <= 4) join_parts<kE4m3 ? 3 : 4, 4>(p, part_0, base, step, count, warp, lane, sh.o[warp], sh.ml[warp]);
+          else join_parts<kE4m3 ? 1 : 2, 8>(p, part_0, base, step, count, warp, lane, sh.o[warp], sh.ml[warp]);
           __syncthreads();
           if (!grouped) {
             merge_warps(finish);

@@ -207,11 +207,14 @@ turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp
   int next_position = t < p.n_tokens ? p.positions[t] : -1, next_seq = t < p.n_tokens ? sequence_of(t) : -1;
   for (; t < p.n_tokens; t += stride) {
     const uint16_t *x = from + t * from_token;
+    auto in_row = [&](int h) {                                 // checked build: a token's row, and this lane's pieces inside it
+      return SAGEKV_OK_INDEX(p.c.status, t < p.n_tokens && h < heads && pa >= 0 && pa + 8 <= kHeadDim && pa + pab >= 0 && pa + pab + 8 <= kHeadDim);
+    };
     uint4 xa[kTurnQuads], xb[kTurnQuads];
     auto load = [&](int h) {
 #pragma unroll
       for (int u = 0; u < kTurnQuads; ++u)
-        if (h + 4 * u < end) {
+        if (h + 4 * u < end && in_row(h + 4 * u)) {
           xa[u] = ld_v4(x);
           xb[u] = ld_v4(x + pab);
           x += from_step;
@@ -227,8 +230,9 @@ turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp
     int64_t row = -1;                                          // where any of position, sequence and page id is out of range: none
     if (kMode != kTurnOnly && kind != 0 && seq >= 0 && seq < p.c.n_seqs && position < p.c.max_pages * p.c.page_size) {
       const int entry = page_of(position, p.c.page_size, p.c.page_magic);
-      row = paged_row(p.c.table[seq * p.c.table_stride + entry], p.c.n_pages, position - entry * p.c.page_size, first, p.c.page_stride,
-                      p.c.head_stride, p.c.token_stride);
+      const int slot = position - entry * p.c.page_size;
+      if (SAGEKV_OK_ENTRY(p.c, seq, entry) && SAGEKV_OK_INDEX(p.c.status, slot >= 0 && slot < p.c.page_size))
+        row = paged_row(p.c.table[seq * p.c.table_stride + entry], p.c.n_pages, slot, first, p.c.page_stride, p.c.head_stride, p.c.token_stride);
     }
     Angles a;
     if (kind != 2 && p.rope.rotary_dim > 0) angles_of(turns, p.rope.amplitude, position, lane, a);
@@ -243,7 +247,7 @@ turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp
         if (h > first) load(h);
 #pragma unroll
         for (int u = 0; u < kTurnQuads; ++u) {
-          if (h + 4 * u >= end) continue;
+          if (h + 4 * u >= end || !in_row(h + 4 * u)) continue;
           f32x2 y[8];
           if (!as_is) {
             rotate(p.rope, a, xa[u], xb[u], y);
@@ -266,7 +270,7 @@ turn_rows_kernel(const __grid_constant__ PagedAppendParams p, const int per_warp
         if (h > first) load(h);
 #pragma unroll
         for (int u = 0; u < kTurnQuads; ++u) {
-          if (h + 4 * u >= end) continue;
+          if (h + 4 * u >= end || !in_row(h + 4 * u)) continue;
           if (as_is) {
             st_v4(o, xa[u]);
             st_v4(o + pab, xb[u]);
@@ -338,13 +342,14 @@ __global__ void __launch_bounds__(kCompactWarps * 32) paged_compact_kernel(const
     const int r = first + lane;
     int tok = r < p.S ? r : p.N - L + r;
     if (r >= p.S && r < p.S + n_sel) {                         // the lists of a KV head's query heads lie one behind the other, as its segments do
-      const int off = p.idx[(int64_t)bk * n_sel + (r - p.S)];
+      const int off = SAGEKV_OK_INDEX(p.c.status, bk < p.B * p.H_kv) ? p.idx[(int64_t)bk * n_sel + (r - p.S)] : -1;
       tok = off >= 0 && off < p.E ? p.S + off : -1;
     }
     if (tok >= 0) {
       const int entry = page_of(tok, p.c.page_size, p.c.page_magic);
-      src = paged_row(p.c.table[(int64_t)b * p.c.table_stride + entry], p.c.n_pages, tok - entry * p.c.page_size, kvh, p.c.page_stride,
-                      p.c.head_stride, p.c.token_stride);
+      const int slot = tok - entry * p.c.page_size;
+      if (SAGEKV_OK_ENTRY(p.c, b, entry) && SAGEKV_OK_INDEX(p.c.status, slot >= 0 && slot < p.c.page_size && kvh < p.H_kv))
+        src = paged_row(p.c.table[(int64_t)b * p.c.table_stride + entry], p.c.n_pages, slot, kvh, p.c.page_stride, p.c.head_stride, p.c.token_stride);
     }
     if (src < 0) atomicOr(p.c.status, kStatusBounds);          // a position or a page id out of range: the row is left as it was
   }

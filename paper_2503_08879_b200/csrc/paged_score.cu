@@ -61,7 +61,8 @@ paged_score_kernel(const ScoreParams p, const PagedView c, const __grid_constant
     if (anew || next - ids_unit >= 32) {
       ids_unit = next;
       const int tile = tile_of(next + lane);
-      ids = tile < end_tile ? table[page_of(tile << 4, c.page_size, c.page_magic)] : -1;
+      const int entry = page_of(tile << 4, c.page_size, c.page_magic);
+      ids = tile < end_tile && SAGEKV_OK_ENTRY(c, b, entry) ? table[entry] : -1;
     }
     const int first = tile_of(next) << 4;
     next_slot = first - page_of(first, c.page_size, c.page_magic) * c.page_size;
@@ -70,7 +71,7 @@ paged_score_kernel(const ScoreParams p, const PagedView c, const __grid_constant
   auto request = [&](int s) {
     if (next >= u_end || tile_of(next) >= end_tile) return;
     const uint32_t bar = bars + 8u * s;
-    if (next_page >= 0 && next_page < c.n_pages) {
+    if (next_page >= 0 && next_page < c.n_pages && SAGEKV_OK_TILE(c, next_slot, kvh, p.H_kv)) {
       absent &= ~(1u << s);
       if (lane == 0) mbar_expect_tx(bar, kTileBytes);
       __syncwarp();
@@ -93,6 +94,7 @@ paged_score_kernel(const ScoreParams p, const PagedView c, const __grid_constant
   if (chunk == 0 && p.sketch_off >= 0) {                       // the rows' histograms are filled by atomic adds in the second pass
     for (int i = threadIdx.x; i < p.G * (kSketchBins + 4); i += kPsThreads) {
       const int h = i / (kSketchBins + 4);
+      if (!SAGEKV_OK_INDEX(p.status, p.sketch_off >= p.E && p.sketch_off + kSketchBins + 4 <= p.row_stride && kvh * p.G + h < p.H_q)) continue;
       reinterpret_cast<uint32_t *>(p.scores + ((int64_t)b * p.H_q + kvh * p.G + h) * p.row_stride + p.sketch_off)[i - h * (kSketchBins + 4)] = 0u;
     }
   }
@@ -125,7 +127,7 @@ paged_score_kernel(const ScoreParams p, const PagedView c, const __grid_constant
     const bool v1 = i1 >= 0 && i1 < p.E && SAGEKV_OK_INDEX(p.status, (int64_t)i1 < p.row_stride);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      if (2 * cc + e >= p.G) continue;
+      if (2 * cc + e >= p.G || !SAGEKV_OK_INDEX(p.status, kvh * p.G + 2 * cc + e < p.H_q && b < p.B)) continue;
       float *row = row0 + e * p.row_stride;
       if (v0) row[i0] = sv[e];
       if (v1) row[i1] = sv[2 + e];
