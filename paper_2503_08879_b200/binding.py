@@ -521,7 +521,7 @@ class SageKV:
         n, heads, d = shape
         if d != 128 or not _placed(_BF16, self.device_index, x, out):
             raise ValueError("expected bf16 rows [tokens, heads, 128] on the context's device")
-        if not _placed_row(_INT32, self.device_index, n, positions, False):
+        if positions is None or not _placed_row(_INT32, self.device_index, n, False, positions):
             raise ValueError("expected contiguous int32 positions on the context's device, one per token")
         code = _marshal.rope(self.ctx, plan, x, n, heads, positions, out)
         if code:
@@ -535,9 +535,9 @@ class SageKV:
         n, heads, d = shape
         device = self.device_index
         if heads != self.shape[1] or d != 128 or v.shape != shape or cache.n_kv_heads != heads or cache.device_index != device or \
-                not _placed(_BF16, device, k, v):
-            raise ValueError("expected bf16 k and v [tokens, H_kv, 128] and pages of H_kv heads on the context's device")
-        if not _placed_row(_INT32, device, n, positions, False) or not (seqs is None or _placed_row(_INT32, device, n, seqs, False)):
+                not _placed(_BF16, device, k, v, q, q_out):
+            raise ValueError("expected bf16 k and v [tokens, H_kv, 128], bf16 q and q_out and pages of H_kv heads on the context's device")
+        if positions is None or not _placed_row(_INT32, device, n, False, positions, seqs):
             raise ValueError("expected contiguous int32 positions and seqs on the context's device, one per token")
         if q is not None:
             shape = q.shape
@@ -545,8 +545,8 @@ class SageKV:
                 q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
             elif q_out is not q and q_out.shape != shape:
                 raise ValueError("expected q_out with the shape of q")
-            if shape != (n, self.shape[0], 128) or not _placed(_BF16, device, q, q_out):
-                raise ValueError("expected bf16 q and q_out [tokens, H_q, 128] on the context's device")
+            if shape != (n, self.shape[0], 128):
+                raise ValueError("expected q [tokens, H_q, 128]")
         code = _marshal.paged_append(self.ctx, cache, k, v, n, positions, seqs, plan, q, q_out)
         if code:
             _check(code, "sagekv_paged_append", self.ctx)
@@ -561,9 +561,9 @@ class SageKV:
         rows = n * shape[1]
         if out is None:
             out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        elif not _placed_row(_BF16, device, rows * 128, out, True):
+        elif not _placed_row(_BF16, device, rows * 128, True, out):
             raise ValueError("expected contiguous bf16 out [n_seqs, H_q, 128] on the context's device")
-        if lse is not None and not _placed_row(_FP32, device, rows, lse, True):
+        if not _placed_row(_FP32, device, rows, True, lse):
             raise ValueError("expected contiguous fp32 lse [n_seqs, H_q] on the context's device")
         code = _marshal.paged_attn(self.ctx, q, cache, out, lse)
         if code:
@@ -573,7 +573,7 @@ class SageKV:
     def paged_score(self, q_last, cache: PagedCache, n_ctx: int, n_init: int, n_recent: int, scores=None):
         """score() on a paged cache whose sequences have n_ctx tokens each."""
         (Hq, Hkv, d, batch), device = self.shape, self.device_index
-        if not _placed_row(_BF16, device, batch * Hq * d, q_last, False) or cache.n_kv_heads != Hkv or cache.device_index != device:
+        if q_last is None or not _placed_row(_BF16, device, batch * Hq * d, False, q_last) or cache.n_kv_heads != Hkv or cache.device_index != device:
             raise ValueError("expected contiguous bf16 q_last [B, H_q, 128] and pages of H_kv heads on the context's device")
         if scores is None:
             scores = self.new_scores(n_ctx, n_init, n_recent)
@@ -592,7 +592,7 @@ class SageKV:
         if cache.n_kv_heads != self.shape[1] or cache.device_index != device:
             raise ValueError("expected pages of H_kv heads on the context's device")
         k_q = max(0, min(k // self.G, n_ctx - 1 - n_init - n_recent))
-        if idx is not None and not _placed_row(_INT32, device, self.shape[3] * self.shape[0] * k_q, idx, False):
+        if not _placed_row(_INT32, device, self.shape[3] * self.shape[0] * k_q, False, idx):
             raise ValueError("expected contiguous int32 lists [B, H_q, min(k / G, E)] on the context's device")
         if layer is None:
             layer = self.new_layer(n_init, n_recent, k)

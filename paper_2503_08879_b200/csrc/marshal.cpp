@@ -340,14 +340,19 @@ PyObject *placed(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return PyBool_FromLong(yes);
 }
 
-// dtype, device, n, tensor, more: is it of that type, on that device, and n elements (or, if `more`, at least n) one behind the other?
+// dtype, device, n, more, tensors: is each (None: passed over) of that type, on that device, and n elements (or, if `more`, at least n) one
+// behind the other?
 PyObject *placed_row(PyObject *, PyObject *const *a, Py_ssize_t n) {
   int64_t device, want, elements, contiguous;
-  bool yes;
-  if (!count(n, 5) || !integer(a[1], &device) || !integer(a[2], &want) || !of_kind(a[3], a[0], device, &yes) || !number(a[3], g_numel, &elements) ||
-      !number(a[3], g_is_contiguous, &contiguous))
-    return nullptr;
-  return PyBool_FromLong(yes && contiguous != 0 && (elements == want || (elements > want && a[4] == Py_True)));
+  if (n < 4) return PyErr_Format(PyExc_TypeError, "expected a type, a device, a number of elements and a truth value");
+  if (!integer(a[1], &device) || !integer(a[2], &want)) return nullptr;
+  bool yes = true;
+  for (Py_ssize_t i = 4; yes && i < n; ++i) {
+    if (a[i] == Py_None) continue;
+    if (!of_kind(a[i], a[0], device, &yes) || !number(a[i], g_numel, &elements) || !number(a[i], g_is_contiguous, &contiguous)) return nullptr;
+    yes = yes && contiguous != 0 && (elements == want || (elements > want && a[3] == Py_True));
+  }
+  return PyBool_FromLong(yes);
 }
 
 // Kc, Vc, batch, heads, rows: are both [batch, heads, at least so many rows, 128], with the same shape and strides?
