@@ -58,8 +58,8 @@ struct PagedAttnParams {
   int32_t *tickets;        // [n_seqs * H_kv], zero between launches
   int32_t *group_tickets;  // [CTAs][2], zero between launches
   int G, H_q, H_kv;
-  int most_ctas, n_tickets;   // extents of the scratch (looked at in the checked build): CTAs with parts and group tickets, pair tickets
   float scale_log2;
+  int most_ctas, n_tickets;   // extents of the scratch (looked at in the checked build): CTAs with parts and group tickets, pair tickets
 };
 cudaError_t launch_paged_attn(const PagedAttnParams &p, int dtype, int n_sm, cudaStream_t stream);
 cudaError_t paged_attn_setup();   // one-time function attributes, with the device current

@@ -98,15 +98,15 @@ __device__ __forceinline__ int places_of(int len) { return len > 0 ? (len + 16 *
 // a head going through sixteen parts at a time: 1.2 at 2 parts, 1.7 at 8, 3.1 at 29, 3.7 at 37.  Six parts at a time instead of four
 // cost registers and with them the loop over the tiles: 8-bit, 8 x 32768 tokens 86.6 -> 90.2)
 template <int kParts, int kHeads>
-__device__ __forceinline__ void join_parts(const PagedAttnParams &p, const float *part_0, int base, int step, int count, int warp, int lane, float *o_to,
-                                           float2 *ml_to) {
+__device__ __forceinline__ void join_parts(const PagedAttnParams &p, const float *part_0, int base, int step, int count, int G, int warp, int lane,
+                                           float *o_to, float2 *ml_to) {
   static_assert(kParts * kHeads <= 32 && (kHeads & (kHeads - 1)) == 0, "a lane per part and head");
   const int u_mine = lane / kHeads, h_mine = lane & (kHeads - 1);   // the lane of part u and head h works out its weight
   float M = -INFINITY, l = 0.f;                              // of head h_mine
   float4 o[kHeads];
 #pragma unroll
   for (int h = 0; h < kHeads; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int G = p.G, part_floats = paged_part_floats(G);
+  const int part_floats = paged_part_floats(G);
   auto part_of = [&](int k) {
     const int i = base + k * step;
     return part_0 + (int64_t)(2 * i + (i == 0 ? 1 : 0)) * part_floats;
@@ -515,8 +515,8 @@ paged_attn_kernel(const PagedAttnParams p, const __grid_constant__ CUtensorMap m
           if (sh.arrived != count - 1) break;                // else every other part is in scratch
           if (tid == 0) *ticket = 0;
           // (beside an 8-bit cache fewer at a time: the loop over the tiles needs the registers, 8 x 32768 tokens 88.7 -> 86.1 us)
-          if (p.G <= 4) join_parts<kE4m3 ? 3 : 4, 4>(p, part_0, base, step, count, warp, lane, sh.o[warp], sh.ml[warp]);
-          else join_parts<kE4m3 ? 1 : 2, 8>(p, part_0, base, step, count, warp, lane, sh.o[warp], sh.ml[warp]);
+          if (p.G <= 4) join_parts<kE4m3 ? 3 : 4, 4>(p, part_0, base, step, count, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
+          else join_parts<kE4m3 ? 1 : 2, 8>(p, part_0, base, step, count, p.G, warp, lane, sh.o[warp], sh.ml[warp]);
           __syncthreads();
           if (!grouped) {
             merge_warps(finish);
