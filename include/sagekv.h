@@ -293,7 +293,9 @@ int sagekv_quest_bounds(sagekv_ctx *ctx, const void *q, const void *kmin, const 
  * (batch*H_q rows of n values, stride scores_row_stride, a multiple of 4; base
  * 16-byte aligned) the min(k_q, n) largest, lower index winning ties, written
  * ascending as 0-based indices to idx [batch*H_q, min(k_q, n)].  n may not exceed
- * the context's max_ctx.  Used for the comparator's block selection.
+ * the context's max_ctx.  The hints of sagekv_set_select_hint do not apply: the
+ * rows are read in every mode.  Used for the comparator's block selection and
+ * for the lists of sagekv_paged_compact.
  * Errors: INVALID, ALIGN, UNSUPPORTED, DEVICE, CUDA. */
 int sagekv_select_topk(sagekv_ctx *ctx, const float *scores, int64_t scores_row_stride, int64_t n,
                        int32_t k_q, int32_t *idx, void *stream);
@@ -560,8 +562,12 @@ int sagekv_paged_attn(sagekv_ctx *ctx, const void *q, int64_t q_stride, const sa
 
 /* sagekv_score on a paged cache: every sequence has n_ctx tokens, and n_seqs
  * must be the context's batch.  Same output (the sums of a product in another
- * order), hints and errors as sagekv_score, plus those of the cache (INVALID also
- * for n_seqs != batch or n_ctx above max_pages * page_size).  From an 8-bit cache
+ * order) and errors as sagekv_score, plus those of the cache (INVALID also
+ * for n_seqs != batch or n_ctx above max_pages * page_size).  The hints of
+ * sagekv_set_select_hint are left behind the rows as sagekv_score leaves them, for a
+ * sagekv_select_compact on the same rows; sagekv_select_topk, whose lists
+ * sagekv_paged_compact takes, does not read them, so there they only cost
+ * time: leave the hint off.  From an 8-bit cache
  * the scores are those of the values it stands for.  Tokens whose page id is out of
  * range get the score 0 (where no token of the region has a page, all get the same)
  * and set the status bit. */

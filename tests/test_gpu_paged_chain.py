@@ -44,3 +44,24 @@ def test_decode_from_an_8_bit_prompt_is_that_from_its_widened_rows(Hq, Hkv, scal
         assert torch.equal(out, want) and torch.equal(lse, plain_lse) and torch.isfinite(out).all()
     assert sk.status() == 0
     sk.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_hints_change_no_list(dtype):
+    """sagekv_select_topk passes over the rows in every hint mode, also of scores that have a histogram or a list behind them."""
+    N, S, R, G, k_q = 20011, 4, 128, 4, 100
+    E = N - 1 - S - R
+    B, sk = context(8, 2, 1, max_ctx=N, max_len=S + G * k_q + R + 1)
+    pool = O.Pool(2, 64, 1, -(-N // 64), dtype, "cuda").fill([N])
+    q = random(1, 8, 128, spread=2.0)
+    for hint in (0, 1, 2):
+        sk.set_select_hint(hint, G * k_q)
+        scores = sk.paged_score(q, pool.cache(B), N, S, R)
+        idx = torch.empty(1, 8, k_q, dtype=torch.int32, device="cuda")
+        B.sagekv_select_topk(sk.ctx, scores, scores.stride(0), E, k_q, idx)
+        want = torch.sort(scores[:, :E], dim=1, descending=True, stable=True).indices[:, :k_q].sort(dim=1).values
+        assert torch.equal(idx[0].long(), want)
+        layer = sk.paged_compact(idx, pool.cache(B), N, S, R, G * k_q)
+        assert layer.state.k_q == k_q
+    assert sk.status() == 0
+    sk.close()
