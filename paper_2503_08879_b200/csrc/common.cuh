@@ -172,9 +172,10 @@ float decode_geometry(int L, int heads, int G, const DeviceInfo *dev, int mode, 
 // ---- status word -------------------------------------------------------------
 // One int32 in device memory per context, OR-ed into by the kernels, read by sagekv_status.
 constexpr int kStatusWaitTimeout = 1;   // a bounded wait on a copy barrier gave up
-constexpr int kStatusBounds = 2;        // checked build: an index outside its buffer was found and the access skipped
+constexpr int kStatusBounds = 2;        // an index outside its buffer was found and the access skipped: of what a paged call reads from device
+                                        // memory (page ids, positions, sequences, lists, lengths) in every build, of any other in the checked build
 
-// In a build with -DSAGEKV_CHECKS every global-memory index of the kernels is compared with the extent the
+// In a build with -DSAGEKV_CHECKS the global-memory indexes of the kernels are compared with the extents the
 // call was given; a violation sets kStatusBounds and the access is skipped (nothing traps).  Otherwise the
 // condition is not evaluated.
 #if defined(SAGEKV_CHECKS)

@@ -1,7 +1,8 @@
 // Attention of one new token per sequence over its whole paged cache.
 //
 //   out[s, h] = sum_t w_t V[t] / sum_t w_t,   w_t = exp(scale <q[s, h], K[t]>),   t < seq_lens[s],
-// K and V of KV head h / G.  The rows are read once, so the floor is HBM: sum of the lengths * H_kv * 2 rows.
+// K and V of KV head h / G.  The rows are read once: sum of the lengths * H_kv * 2 rows out of HBM.  ("Bytes" below is that at the rate of a
+// copy, which a stream that only reads may pass by a few per cent.)
 //
 // Split.  The lengths are known on the device only (a captured launch serves later lengths), and a batch may be one
 // long sequence or many uneven ones.  So all (sequence, KV head) pairs form one list of units of six 16-token tiles, a
@@ -18,12 +19,16 @@
 // reduced cache: S = K Q^T with tokens as rows (M = 16) and the heads as columns (N = 8), O^T += V^T P.  An 8-bit cache is
 // staged as it is and widened to f16 (exact) between shared memory and the tensor cores.
 //
+// The weights are rounded to the 16 bits that the second product takes, bf16 or, beside an 8-bit cache, f16; the sum beneath the line is
+// that of the unrounded ones.  At 131072 tokens that brings the result from 1.66e-3 of its norm (its own rounding to bf16) to 1.76e-3; two
+// halves of a weight would double the second product.
+//
 // What bounds it.  Long caches: HBM.  Twelve warps per SM with 8 KB on the way each are enough; more bytes in flight only let some
 // SMs have more of the bandwidth than others, and the launch waits for the others (us, 8 heads x 131072 tokens / x 8
-// sequences of 32768 / 8-bit; floors 81.8 / 163.5 / 40.9, 81.8): eight warps with 24 KB each 94.6 / 171 / 59.4, 101; with 16 KB
+// sequences of 32768 / 8-bit; bytes 81.8 / 163.5 / 40.9, 81.8): eight warps with 24 KB each 94.6 / 171 / 59.4, 101; with 16 KB
 // 89.9 / 170 / 55.5, 99.6; twelve with 8 KB 82.8 / 161 / 46.5, 86; sixteen (128 registers) 93.6 / 168 / 53.6, 94.2.  Short ones: a chain of waits
 // (us in a launch on 8 heads x 300 tokens, 5.9 in all): the previous launch's end seen 1.1, lengths 0.6, page ids and copies issued
-// 0.9, rows there 0.4, a tile and the warps' merge 1.1, ticket 0.9, join 1.2.  Between them both (8 heads x 8192 tokens: 12.2, floor 5.1).
+// 0.9, rows there 0.4, a tile and the warps' merge 1.1, ticket 0.9, join 1.2.  Between them both (8 heads x 8192 tokens: 12.3, bytes 5.1).
 //
 // A tile's rows behind the sequence's end hold anything: their scores are replaced, not added to, and their V rows are
 // cleared in the fragments, since zero times NaN is NaN.

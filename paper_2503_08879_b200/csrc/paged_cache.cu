@@ -2,7 +2,8 @@
 //   rope      rows of queries or keys rotated by their positions;
 //   append    keys and values of new tokens into their pages, the keys rotated on the way, the tokens' queries beside;
 //   compact   Step 3 on pages: the reduced cache from the kept positions.
-// All are bound by memory: every row is read once and written once, 16 bytes per access.
+// Every row is read once and written once, 16 bytes per access (8 where a row is stored in 8 bits).  Many rows are bound by HBM, those
+// that enter an 8-bit cache nearly as much by the issue rate; few rows by latency.
 #include "paged.cuh"
 
 namespace sagekv {
@@ -177,8 +178,8 @@ enum { kTurnOnly = 0, kTurnAppend = 1, kTurnAppendE4m3 = 2 };
 
 // A warp takes rows of one kind (queries, keys or values; all of a token's, or some groups of four of them: blockIdx.y says which) of
 // one token after another.  The rows are on their way while position and page are looked up.
-// Bound by HBM where there are many tokens of bf16 (65536 x 8 KV heads 85.3 us, floor 81.8; 20011 x 28 heads rotated alone 46.3 of 43.7),
-// close to the issue rate into an 8-bit cache (73 us of 61.4: conversions and the angles against half the bytes), by latency where
+// Bound by HBM where there are many tokens of bf16 (in a graph 65536 x 8 KV heads 85.4 us, floor 81.8; 20011 x 28 heads rotated alone 46.5 of 43.7),
+// close to the issue rate into an 8-bit cache (73.1 us of 61.4: conversions and the angles against half the bytes), by latency where
 // there are few (one token 2 us).  What it took (us, 65536 tokens x 8 KV heads, bf16 / 8-bit): a warp for all rows of a token
 // 122.7 / 124.7 (1080 instructions a token); loads and angles shared out leaner, a kind per warp 100.7 / 98.6; frequencies
 // through shared memory 90.3 / 84.1; sines from the quadrant, packed instructions 88.3 / 80.4; from token to token in 72 registers
@@ -318,9 +319,9 @@ cudaError_t launch_paged_append(const PagedAppendParams &p, int dtype, int n_sm,
 // each lane finds one row's place (list, then table: two loads one behind the other, for all rows at once), then the
 // rows are moved kRows at a time, 16 bytes per lane, all loads ahead of the stores.  An 8-bit row is widened: code * scale,
 // rounded to bf16.  Bound by that chain of loads where the rows are few, by their scatter where they are many.  (us, 8 heads x 2049 bf16
-// rows / 16 x 8193 bf16 / 16 x 8193 8-bit; floors 2.6 / 20.5 / 15.4: eight rows at once in blocks of eight warps, loads past L1
+// rows / 16 x 8193 bf16 / 16 x 8193 8-bit in a graph, the first with its rows in L2; bytes at the copy rate 2.6 / 20.5 / 15.4: eight rows at once in blocks of eight warps, loads past L1
 // 5.25 / 35.9 / 24.9, four in blocks of four 4.1 / 25.1 / 25.6, plain loads besides 3.5 / 24.0 / 25.5; 8-bit eight at once and 32 per
-// warp 23.3, with stores of whole sectors 20.4, 16 per warp 19.1; bf16 now 3.4 / 23.7)
+// warp 23.3, with stores of whole sectors 20.4, 16 per warp 19.1; bf16 now 3.4 / 23.7.  The first out of HBM, layer after layer: 5.8)
 constexpr int kCompactWarps = 4;
 
 template <bool kE4m3, int kRows>

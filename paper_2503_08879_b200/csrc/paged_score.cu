@@ -4,9 +4,9 @@
 // matrix fragments; here every sequence has the same length, so a KV head's tiles are simply dealt to `n_chunks` CTAs, and in
 // a CTA to its warps in turn.  A warp's page ids are looked up 32 tiles at a time.  (Loading the rows straight into
 // fragments, as the score step without pages does, puts the look-up in front of every CTA's loads: both passes on 131072
-// tokens x 8 heads 59.6 us, this 47.3.)  Writes the scaled logits and a (max, sum) pair per CTA and head; the second pass is the
+// tokens x 8 heads 59.6 us, this 48.1.)  Writes the scaled logits and a (max, sum) pair per CTA and head; the second pass is the
 // score step's own, 7 us of those.  Bound by HBM, K being read once, and like the attention served best by few bytes in flight (us, bf16 / 8-bit
-// cache: 18 warps per SM with 8 KB each 50.1 / 35.0, 24 with 8 KB 50.2 / 36.0, 24 with 4 KB 48.3 / 33.6).
+// cache: 18 warps per SM with 8 KB each 50.1 / 35.0, 24 with 8 KB 50.2 / 36.0, 24 with 4 KB 48.1 / 34.2).
 #include "paged_tiles.cuh"
 
 namespace sagekv {
@@ -16,7 +16,6 @@ constexpr int kPsThreads = kPsWarps * 32;
 constexpr int kPsRingBytes = kSlotBytes;        // per warp: one stage of bf16 tiles, or two of 8-bit ones
 constexpr int kPsCtasPerSm = 3;
 constexpr int kPsMaxStages = 2;
-constexpr int kPsMinUnits = 1;                  // a CTA's least share: a tile per warp
 
 struct PsShared {
   unsigned char ring[kPsWarps][kPsRingBytes];   // boxes with the 128-byte swizzle: 1024-byte boundaries
@@ -173,7 +172,7 @@ cudaError_t launch_paged_score(ScoreParams p, const PagedView &c, int dtype, int
   // one wave of CTAs; with so many heads that fewer than four would share one, eight each: the waves then even out
   const int heads = p.B * p.H_kv, wave = kPsCtasPerSm * n_sm;
   int ctas = heads > wave / 4 ? 8 : wave / heads;
-  if (ctas > (n_units + kPsMinUnits - 1) / kPsMinUnits) ctas = (n_units + kPsMinUnits - 1) / kPsMinUnits;
+  if (ctas > n_units) ctas = n_units;                          // a CTA's least share: a tile per warp
   if (ctas > max_chunks) ctas = max_chunks;
   const int per_cta = (n_units + ctas - 1) / ctas;
   p.n_chunks = (n_units + per_cta - 1) / per_cta;
