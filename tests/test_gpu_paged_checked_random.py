@@ -19,5 +19,5 @@ def test_random_paged_cases_on_the_checked_build():
                            cwd=ROOT, env=env, capture_output=True, text=True)
     assert probe.returncode == 0 and probe.stdout.strip() == "1", probe.stderr[-2000:]
     res = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-m", "gpu", "tests/test_gpu_paged_fuzz.py", "tests/test_gpu_paged_absent.py",
-                          "tests/test_gpu_paged_limits.py"], cwd=ROOT, env=env, capture_output=True, text=True)
+                          "tests/test_gpu_paged_limits.py", "tests/test_gpu_paged_edges.py"], cwd=ROOT, env=env, capture_output=True, text=True)
     assert res.returncode == 0, (res.stdout[-3000:], res.stderr[-2000:])
