@@ -112,7 +112,7 @@ paged_score_kernel(const ScoreParams p, const PagedView c, const __grid_constant
     float sv[4];
     if (!mbar_wait(bars + 8u * stage, phase)) timed_out = true;
     if ((absent >> stage) & 1u) {                              // tokens that are not there get no weight; a row without any stays finite
-      sv[0] = sv[1] = sv[2] = sv[3] = -1.0e30f;
+      sv[0] = sv[1] = sv[2] = sv[3] = -3.40282347e38f;         // (the lowest number: no logit is below it)
     } else {
       score_tile<kE4m3>(ring + (uint32_t)(stage * kTileBytes), k_off, qb, mult0, mult1, sv);
     }

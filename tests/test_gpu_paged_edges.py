@@ -159,3 +159,23 @@ def test_decode_ahead_of_its_wait_behind_the_paged_calls(mode, dtype):
         same()
     assert sk.status() == 0
     sk.close()
+
+
+def test_absent_tokens_weigh_nothing_beside_the_lowest_logits():
+    """Logits of -10^32: a token whose page is none still gets no weight, and those that are there share it."""
+    N, S, R = 208, 0, 15
+    E = N - 1 - S - R
+    B, sk = context(1, 1, 1, max_ctx=N)
+    pool = O.Pool(1, 16, 1, 13, BF16, "cuda").fill([N])
+    pool.k.zero_()
+    pool.k[..., 0] = -2.0 ** 50
+    q = torch.zeros(1, 1, 128, dtype=BF16, device="cuda")
+    q[..., 0] = 2.0 ** 60
+    pool.table[0, 2] = -1
+    p = sk.paged_score(q, pool.cache(B), N, S, R)[0, :E]
+    with pytest.raises(B.SagekvError):
+        sk.status()
+    gone = torch.zeros(E, dtype=torch.bool, device="cuda")
+    gone[32:48] = True
+    assert not p[gone].any() and torch.allclose(p[~gone], torch.full_like(p[~gone], 1 / (E - 16)), rtol=1e-5)
+    sk.close()
