@@ -419,7 +419,7 @@ int sagekv_score_static(const sagekv_shape *shape, const void *q_last, const voi
  * sagekv_paged_check): INVALID (null, sizes or strides too small, an unknown
  * dtype), ALIGN, UNSUPPORTED (page_size % 16, n_seqs above the batch,
  * max_pages * page_size above 2^30, n_seqs * H_kv * max_pages * page_size / 16
- * above 2^31 - 1, page_stride of 2^40 bytes or more). */
+ * above 2^31 - 1, a stride of 2^40 bytes or more). */
 enum { SAGEKV_CACHE_BF16 = 0, SAGEKV_CACHE_E4M3 = 1 };
 
 typedef struct {
